@@ -299,6 +299,53 @@ int bf1_plan_route_shard_strided(int64_t n_tokens, int32_t first_block, int32_t 
                                  int32_t *cu_seqlens_out_dev, void *stream);
 
 
+/* ---- rotary positions ------------------------------------------------------------------------------------
+ * (No counterpart in the paper, whose model applies them in front of the operator: Section 4.1's geometry.)
+ * The first `dim` of a head's d dimensions are dim / 2 pairs (x, y); at position p pair i becomes
+ *      magnitude * (x cos a - y sin a, x sin a + y cos a),   a = 2 pi * turns[i] * p,
+ * the other d - dim are carried over.  The angle is formed in 64 bits, so that far positions keep their place on the circle. */
+enum { BF1_ROPE_HALF = 0,           /* pair i is (x[i], x[i + dim / 2])                            */
+       BF1_ROPE_INTERLEAVED = 1 };  /* pair i is (x[2 i], x[2 i + 1])                              */
+enum { BF1_ROPE_NONE = 0,           /* turns[i] = base^(-2 i / dim) / (2 pi)                       */
+       BF1_ROPE_LINEAR = 1,         /* those, divided by `factor`                                  */
+       BF1_ROPE_NTK = 2,            /* those of the base base * factor^(dim / (dim - 2))           */
+       BF1_ROPE_YARN = 3 };         /* by turns over the original length, n = original_len * turns[i]: as they are where
+                                       n >= beta_fast, divided by `factor` where n <= beta_slow, mixed linearly in n
+                                       between; magnitude 0.1 ln(factor) + 1                       */
+typedef struct {
+    int32_t dim;            /* rotated dimensions: a multiple of 16                                */
+    int32_t scaling;        /* BF1_ROPE_NONE .. BF1_ROPE_YARN                                      */
+    double base;            /* above 1                                                             */
+    double factor;          /* >= 1; not read by BF1_ROPE_NONE                                     */
+    double original_len, beta_fast, beta_slow;   /* BF1_ROPE_YARN                                  */
+} bf1_rope_cfg;
+typedef struct {
+    int32_t dim;            /* a multiple of 16, at most d                                         */
+    int32_t layout;         /* BF1_ROPE_HALF or BF1_ROPE_INTERLEAVED                               */
+    float magnitude;
+    const double *turns;    /* device [dim / 2]                                                    */
+} bf1_rope;
+
+/* Rows of heads, bf16, the dimensions of a head side by side: head h of token t is at data + t * row_stride + h * head_stride.
+ * Strides are in elements and steps of 8, `data` is 16-byte aligned.  A part of a fused projection's output is such a tensor,
+ * and so is one that lies head by head. */
+typedef struct {
+    void *data;
+    int64_t row_stride, head_stride;
+} bf1_rows;
+
+/* The table of a rope (host only): turns[dim / 2] and the magnitude for bf1_rope. */
+int bf1_rope_turns(const bf1_rope_cfg *cfg /* host */, double *turns /* host out */, double *magnitude /* host out */);
+
+/* Rotates the hq query heads and hkv key heads of `tokens` tokens (hkv = 0: there are no keys; k and out_k are not read).
+ *   positions_dev  device int32 [tokens]; a token of negative position is padding: its output rows are not written
+ *   out_q, out_k   the inputs themselves (same data, same strides) or rows that do not overlap them
+ * bf1_rope_bwd takes the gradients of the rotated heads and gives those of the heads before the rotation. */
+int bf1_rope_fwd(const bf1_rows *q, const bf1_rows *k, const int32_t *positions_dev, int32_t tokens, int32_t hq, int32_t hkv,
+                 int32_t d, const bf1_rope *rope /* host */, const bf1_rows *out_q, const bf1_rows *out_k, void *stream);
+int bf1_rope_bwd(const bf1_rows *d_q, const bf1_rows *d_k, const int32_t *positions_dev, int32_t tokens, int32_t hq, int32_t hkv,
+                 int32_t d, const bf1_rope *rope /* host */, const bf1_rows *out_q, const bf1_rows *out_k, void *stream);
+
 /* Message for the last non-OK status returned on the calling thread ("" if none). */
 const char *bf1_last_error(void);
 

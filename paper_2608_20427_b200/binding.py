@@ -26,6 +26,7 @@ EXPORTS = ("bf1_route_capacity", "bf1_plan_route", "bf1_attn_fwd", "bf1_dense_ca
            "bf1_attn_fwd_noalloc", "bf1_plan_decode", "bf1_decode_workspace_bytes", "bf1_decode_fwd",
            "bf1_attn_bwd", "bf1_attn_bwd_workspace_bytes", "bf1_shard_needed_blocks", "bf1_plan_route_shard",
            "bf1_shard_needed_blocks_strided", "bf1_plan_route_shard_strided",
+           "bf1_rope_turns", "bf1_rope_fwd", "bf1_rope_bwd",
            "bf1_last_error", "bf1_version")
 
 
@@ -52,6 +53,22 @@ class _DecodePlanC(ctypes.Structure):
     """Mirror of bf1_decode_plan."""
     _fields_ = [("max_degree", ctypes.c_int32), ("count", ctypes.c_void_p), ("page", ctypes.c_void_p),
                 ("block", ctypes.c_void_p), ("status", ctypes.c_void_p)]
+
+
+class _RopeCfgC(ctypes.Structure):
+    """Mirror of bf1_rope_cfg."""
+    _fields_ = [("dim", ctypes.c_int32), ("scaling", ctypes.c_int32), ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("original_len", ctypes.c_double), ("beta_fast", ctypes.c_double), ("beta_slow", ctypes.c_double)]
+
+
+class _RopeC(ctypes.Structure):
+    """Mirror of bf1_rope."""
+    _fields_ = [("dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("magnitude", ctypes.c_float), ("turns", ctypes.c_void_p)]
+
+
+class _RowsC(ctypes.Structure):
+    """Mirror of bf1_rows."""
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
 
 
 class Bf1Error(RuntimeError):
@@ -104,6 +121,12 @@ def load():
     L.bf1_plan_route_shard_strided.restype = ctypes.c_int
     L.bf1_plan_route_shard_strided.argtypes = [i64, i32, i32, i32, ctypes.POINTER(RouteCfg), vp, i32, ctypes.POINTER(_RouteC),
                                                vp, vp]
+    rows, ropep = ctypes.POINTER(_RowsC), ctypes.POINTER(_RopeC)
+    L.bf1_rope_turns.restype = ctypes.c_int
+    L.bf1_rope_turns.argtypes = [ctypes.POINTER(_RopeCfgC), ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double)]
+    for name in ("bf1_rope_fwd", "bf1_rope_bwd"):
+        getattr(L, name).restype = ctypes.c_int
+        getattr(L, name).argtypes = [rows, rows, vp, i32, i32, i32, i32, ropep, rows, rows, vp]
     L.bf1_last_error.restype = ctypes.c_char_p
     L.bf1_last_error.argtypes = []
     L.bf1_version.restype = ctypes.c_int
@@ -309,6 +332,75 @@ def attn_bwd(q, k, v, o, lse, d_o, cu_seqlens, max_seqlen: int, route: Route, sc
         workspace = bwd_workspace(route, q.shape[0], q.shape[1], k.shape[1], q.shape[2], q.device)
     return _host().backward(q, k, v, o, lse, d_o, cu_seqlens, max_seqlen, ctypes.addressof(route.c), scale, workspace,
                             _stream_ptr(stream))
+
+
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
+
+
+@dataclass(frozen=True)
+class RopeCfg:
+    """Rotary positions on the first `dim` dimensions of a head (a multiple of 16).
+
+    layout      "half": pair i is (x[i], x[i + dim/2]); "interleaved": (x[2i], x[2i+1])
+    scaling     "none", "linear" (angles / factor), "ntk" (the base times factor^(dim/(dim-2))), "yarn" (angles / factor for pairs
+                that turn at most beta_slow times in original_len tokens, as they are for those that turn beta_fast times or
+                more, linear in the number of turns between; values times 0.1 ln(factor) + 1)
+    magnitude   factor on the rotated values in place of the scaling's own
+    """
+    dim: int
+    base: float = 10000.0
+    layout: str = "half"
+    scaling: str = "none"
+    factor: float = 1.0
+    original_len: float = 0.0
+    beta_fast: float = 32.0
+    beta_slow: float = 1.0
+    magnitude: Optional[float] = None
+
+
+@dataclass
+class Rope:
+    """The device table of a rope: turns per position of every pair, in 64 bits."""
+    dim: int
+    layout: str
+    magnitude: float
+    turns: torch.Tensor
+    c: _RopeC = None
+
+    @staticmethod
+    def from_turns(turns, layout: str, magnitude: float, device) -> "Rope":
+        """A rope of the caller's own frequencies: `turns` of a pair per position (radians / 2 pi), [dim / 2]."""
+        if layout not in ROPE_LAYOUTS:
+            raise ValueError("layout %r: one of %s" % (layout, ", ".join(ROPE_LAYOUTS)))
+        turns = torch.as_tensor(turns, dtype=torch.float64).to(device).contiguous()
+        if turns.dim() != 1 or turns.numel() < 8 or turns.numel() % 8:
+            raise ValueError("turns must be 1-d, 8 pairs at a time")
+        r = Rope(2 * turns.numel(), layout, float(magnitude), turns)
+        r.c = _RopeC(r.dim, ROPE_LAYOUTS[layout], r.magnitude, turns.data_ptr())
+        return r
+
+
+def plan_rope(cfg: RopeCfg, device) -> Rope:
+    """bf1_rope_turns: the table of a rope, made once and used by every layer."""
+    if cfg.scaling not in ROPE_SCALINGS:
+        raise ValueError("scaling %r: one of %s" % (cfg.scaling, ", ".join(ROPE_SCALINGS)))
+    c = _RopeCfgC(cfg.dim, ROPE_SCALINGS[cfg.scaling], cfg.base, cfg.factor, cfg.original_len, cfg.beta_fast, cfg.beta_slow)
+    turns, magnitude = (ctypes.c_double * max(cfg.dim // 2, 1))(), ctypes.c_double(1.0)
+    _check(load().bf1_rope_turns(ctypes.byref(c), turns, ctypes.byref(magnitude)))
+    return Rope.from_turns(list(turns), cfg.layout, magnitude.value if cfg.magnitude is None else cfg.magnitude, device)
+
+
+def rope_fwd(q, k, positions, rope: Rope, out_q=None, out_k=None, stream=None):
+    """bf1_rope_fwd: (q, k) with their heads rotated to `positions` (int32, one per token; negative: padding, whose output rows
+    are not written).  q [T, hq, d], k [T, hkv, d] or None, bf16; rows and heads may be strided (parts of one projection's output), the
+    outputs too, and they may be the inputs themselves.  Without out_q / out_k new contiguous tensors are made."""
+    return _host().rope(0, q, k, positions, ctypes.addressof(rope.c), rope.turns, out_q, out_k, _stream_ptr(stream))
+
+
+def rope_bwd(d_q, d_k, positions, rope: Rope, out_q=None, out_k=None, stream=None):
+    """bf1_rope_bwd: the gradients of q and k before the rotation, from those behind it.  Arguments as rope_fwd."""
+    return _host().rope(1, d_q, d_k, positions, ctypes.addressof(rope.c), rope.turns, out_q, out_k, _stream_ptr(stream))
 
 
 def shard_needed_blocks(n_tokens: int, lo_block: int, hi_block: int, cfg: Optional[RouteCfg] = None):

@@ -10,8 +10,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libbf1.so")
 HOST_SOURCE = os.path.join(CSRC, "bf1_host.cpp")
-SOURCES = ["bf1_plan.cu", "bf1_attn.cu", "bf1_noalloc.cu", "bf1_decode.cu", "bf1_bwd.cu", "bf1_shard.cu"]
-HEADERS = ["bf1_common.cuh", os.path.join("..", "..", "include", "bf1.h")]
+SOURCES = ["bf1_plan.cu", "bf1_attn.cu", "bf1_noalloc.cu", "bf1_decode.cu", "bf1_bwd.cu", "bf1_shard.cu",
+           "bf1_rope.cu"]
+HEADERS = ["bf1_common.cuh", "bf1_rope.cuh", os.path.join("..", "..", "include", "bf1.h")]
 
 
 def _nvcc() -> str:
@@ -61,7 +62,7 @@ def host_path() -> str:
 def build_host(force: bool = False) -> str:
     """Compile the extension module that marshals torch tensors into the C ABI, if there is none for this torch and Python or it
     is older than its source; return its path.  It links libbf1.so from its own folder, which has to be there already."""
-    deps = [HOST_SOURCE, os.path.join(CSRC, HEADERS[1])]
+    deps = [HOST_SOURCE, os.path.join(CSRC, HEADERS[-1])]
     host = host_path()
     if not force and os.path.exists(host) and all(os.path.getmtime(d) <= os.path.getmtime(host) for d in deps):
         return host

@@ -12,6 +12,7 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -82,6 +83,32 @@ PyObject* pair(const at::Tensor& a, const at::Tensor& b) {
     Py_XDECREF(x);
     Py_XDECREF(y);
     return t;
+}
+
+// Where a call runs: on the device of its tensors, on `stream` or, if that is None, on the device's current stream; what it
+// allocates belongs to that stream.
+struct Place {
+    c10::cuda::CUDAGuard device;
+    c10::cuda::OptionalCUDAStreamGuard guard;
+    void* stream;
+    Place(const at::Tensor& t, PyObject* o) : device((require(t.is_cuda(), "the tensors have to be on a CUDA device"), t.device())) {
+        if (o == Py_None) {
+            stream = c10::cuda::getCurrentCUDAStream(t.device().index()).stream();
+        } else {
+            stream = address<void>(o);
+            guard.reset_stream(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(stream), t.device().index()));
+        }
+    }
+};
+// [tokens, heads, d] bf16 with the dimensions of a head side by side, on `like`'s device
+bf1_rows rows_of(const at::Tensor& t, const at::Tensor& like, const char* what) {
+    require(t.device() == like.device() && t.scalar_type() == at::kBFloat16 && t.dim() == 3 && (t.size(2) == 1 || t.stride(2) == 1), what);
+    return {t.data_ptr(), t.size(0) > 1 ? t.stride(0) : 0, t.size(1) > 1 ? t.stride(1) : 0};
+}
+template <typename T>
+T* array_of(const at::Tensor& t, const at::Tensor& like, at::ScalarType type, const char* what) {
+    require(t.device() == like.device() && t.scalar_type() == type && t.is_contiguous(), what);
+    return static_cast<T*>(t.data_ptr());
 }
 
 struct Qkv {
@@ -206,6 +233,39 @@ PyObject* decode(PyObject* const* a) {
     return pair(out, lse);
 }
 
+// The table of a rope has to lie where the call runs.
+void check_table(const at::Tensor& turns, const at::Tensor& like) {
+    array_of<const double>(turns, like, at::kDouble, "the rope's table must be on the device of the tensors");
+}
+
+// rope(backward, q, k*, positions, rope address, its table, out_q*, out_k*, stream*)
+PyObject* rope(PyObject* const* a) {
+    const bool back = integer(a[0]) != 0, keys = a[2] != Py_None;
+    const at::Tensor &q = tensor(a[1]), &k = keys ? tensor(a[2]) : q, &pos = tensor(a[3]);
+    const auto* table = address<const bf1_rope>(a[4]);
+    const char* const what = "q, k and their outputs must be 3-d bf16 tensors on one CUDA device, the last dimension contiguous";
+    const Place place(q, a[8]);
+    check_table(tensor(a[5]), q);
+    const bf1_rows qr = rows_of(q, q, what), kr = rows_of(k, q, what);
+    require(k.size(0) == q.size(0) && k.size(2) == q.size(2), "q and k must have the same tokens and head dimension");
+    const auto* pp = array_of<const int32_t>(pos, q, at::kInt, "positions must be a contiguous int32 tensor on the same device");
+    require(pos.dim() == 1 && pos.size(0) == q.size(0), "positions must have an entry for every token");
+    const at::Tensor out_q = a[6] == Py_None ? at::empty(q.sizes(), q.options()) : tensor(a[6]);
+    const at::Tensor out_k = !keys ? out_q : a[7] == Py_None ? at::empty(k.sizes(), k.options()) : tensor(a[7]);
+    require(out_q.sizes() == q.sizes() && out_k.sizes() == (keys ? k : q).sizes(), "the outputs must have the shapes of q and k");
+    const bf1_rows oq = rows_of(out_q, q, what), ok = rows_of(out_k, q, what);
+    const int32_t tokens = q.size(0), hq = q.size(1), hkv = keys ? k.size(1) : 0, d = q.size(2);
+    call([&] {
+        return back ? bf1_rope_bwd(&qr, &kr, pp, tokens, hq, hkv, d, table, &oq, &ok, place.stream)
+                    : bf1_rope_fwd(&qr, &kr, pp, tokens, hq, hkv, d, table, &oq, &ok, place.stream);
+    });
+    if (keys) return pair(out_q, out_k);
+    PyObject* x = THPVariable_Wrap(out_q);
+    PyObject* t = x ? PyTuple_Pack(2, x, Py_None) : nullptr;
+    Py_XDECREF(x);
+    return t;
+}
+
 // Argument count, C++ and torch exceptions.
 template <PyObject* (*F)(PyObject* const*), int kArgs>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -237,6 +297,7 @@ PyMethodDef g_methods[] = {
     BF1_ENTRY(backward, 12),
     BF1_ENTRY(plan_decode, 5),
     BF1_ENTRY(decode, 10),
+    BF1_ENTRY(rope, 9),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_host", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

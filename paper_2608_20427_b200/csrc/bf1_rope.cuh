@@ -1,0 +1,115 @@
+// Rotary positions: what the rotation kernel (bf1_rope.cu) and the cache write (bf1_cache.cu), which rotates on the way into
+// the pages, share.
+#pragma once
+
+#include "bf1_common.cuh"
+
+namespace bf1 {
+
+// The tables of a bf1_rope as a kernel takes them.
+struct RopeTable {
+    const double* turns;   // [dim / 2]: turns of a pair per position
+    int32_t dim;           // rotated dimensions of a head; 0: nothing is rotated
+    int32_t half;          // 1: pairs (i, i + dim / 2); 0: pairs (2 i, 2 i + 1)
+    float magnitude;       // factor on the rotated values
+};
+
+// (cos, sin) of a pair's angle, times the magnitude.  The angle is position * turns in 64 bits, of which only the part of a turn
+// counts: exact to 2^-53 of the whole, so that a position of 2^31 still has 1e-7 of a radian, where 32 bits lose all of it
+// beyond 2^24 turns.
+__device__ __forceinline__ float2 rope_angle(const RopeTable& r, int position, int pair) {
+    double t = (double)position * r.turns[pair];
+    t -= rint(t);
+    float s, c;
+    sincospif(2.f * (float)t, &s, &c);
+    return make_float2(c * r.magnitude, s * r.magnitude);
+}
+
+__device__ __forceinline__ void unpack_bf16x8(const uint4& v, float (&x)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ uint4 pack_bf16x8(const float (&x)[8]) {
+    return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+}
+
+// Rows of heads in global memory: bf16, the dimensions of a head side by side, strides in elements.
+struct Rows {
+    __nv_bfloat16* p;
+    int64_t row, head;
+    __device__ __forceinline__ __nv_bfloat16* at(int64_t token, int h) const { return p + token * row + h * head; }
+};
+
+// Sixteen dimensions of one token for heads h0, h0 + step, ... below `heads`: the eight pairs 8 c .. 8 c + 7 where c < dim / 16, or
+// else sixteen dimensions that are carried over.  The angles are made once and serve all of these heads; kAhead heads are asked for
+// before the first is turned.  sign -1 turns back, which is the gradient (a rotation's transpose; the magnitude stays).
+template <int kAhead>
+__device__ __forceinline__ void rope_heads(const RopeTable& r, int position, int64_t token, int c, float sign, const Rows& in_q,
+                                           const Rows& in_k, const Rows& out_q, const Rows& out_k, int hq, int heads, int h0, int step) {
+    const bool turn = 16 * c < r.dim;
+    const int lo = turn && r.half ? 8 * c : 16 * c, hi = turn && r.half ? r.dim / 2 + 8 * c : 16 * c + 8;
+    float cs[8], sn[8];
+    if (turn) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float2 a = rope_angle(r, position, 8 * c + i);
+            cs[i] = a.x;
+            sn[i] = a.y * sign;
+        }
+    }
+    for (int h = h0; h < heads; h += kAhead * step) {
+        uint4 a[kAhead], b[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int hh = h + u * step;
+            if (hh >= heads) break;
+            const __nv_bfloat16* x = hh < hq ? in_q.at(token, hh) : in_k.at(token, hh - hq);
+            a[u] = *reinterpret_cast<const uint4*>(x + lo);
+            b[u] = *reinterpret_cast<const uint4*>(x + hi);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int hh = h + u * step;
+            if (hh >= heads) break;
+            __nv_bfloat16* y = hh < hq ? out_q.at(token, hh) : out_k.at(token, hh - hq);
+            if (turn) {
+                float x0[8], x1[8];
+                unpack_bf16x8(a[u], x0);
+                unpack_bf16x8(b[u], x1);
+                if (r.half) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float p = x0[i], q = x1[i];
+                        x0[i] = p * cs[i] - q * sn[i];
+                        x1[i] = p * sn[i] + q * cs[i];
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float p = x0[2 * i], q = x0[2 * i + 1], s = x1[2 * i], t = x1[2 * i + 1];
+                        x0[2 * i] = p * cs[i] - q * sn[i];
+                        x0[2 * i + 1] = p * sn[i] + q * cs[i];
+                        x1[2 * i] = s * cs[4 + i] - t * sn[4 + i];
+                        x1[2 * i + 1] = s * sn[4 + i] + t * cs[4 + i];
+                    }
+                }
+                a[u] = pack_bf16x8(x0);
+                b[u] = pack_bf16x8(x1);
+            }
+            *reinterpret_cast<uint4*>(y + lo) = a[u];
+            *reinterpret_cast<uint4*>(y + hi) = b[u];
+        }
+    }
+}
+
+// Host checks of a bf1_rope and of rows of heads (bf1_rope.cu).
+int check_rope(const bf1_rope* rope, int32_t d);
+int check_rows(const bf1_rows* rows, const char* name);
+inline Rows rows_of(const bf1_rows* r) { return {static_cast<__nv_bfloat16*>(r->data), r->row_stride, r->head_stride}; }
+inline RopeTable table_of(const bf1_rope* r) { return {r->turns, r->dim, r->layout == BF1_ROPE_HALF ? 1 : 0, r->magnitude}; }
+
+}  // namespace bf1
