@@ -346,6 +346,62 @@ int bf1_rope_fwd(const bf1_rows *q, const bf1_rows *k, const int32_t *positions_
 int bf1_rope_bwd(const bf1_rows *d_q, const bf1_rows *d_k, const int32_t *positions_dev, int32_t tokens, int32_t hq, int32_t hkv,
                  int32_t d, const bf1_rope *rope /* host */, const bf1_rows *out_q, const bf1_rows *out_k, void *stream);
 
+/* ---- filling the paged cache ---------------------------------------------------------------------------------
+ * A serving step adds new_lens[s] tokens to sequence s (prompts and single tokens alike, packed as usual; 0: none; -1: the sequence is
+ * done and gives its pages back).  bf1_plan_cache turns these lengths into all that the step's other calls look up, on the
+ * device, so that a step can be captured into a graph: it takes pages from a stack of free ones, writes them into the page
+ * table, and says where every token stands.  bf1_cache_write then puts a layer's keys and values there.  Pages are 64 tokens. */
+typedef struct {
+    int32_t  batch;             /* host: sequences, at most 65535                                               */
+    int32_t  capacity_tokens;   /* host: rows of the step's packed tensors; the tokens may be fewer             */
+    int32_t  capacity_units;    /* host: bf1_cache_plan_units(batch, capacity_tokens) or more                   */
+    int32_t *seqlens;           /* [batch] cached tokens after the step; may be seqlens_dev itself              */
+    int32_t *free_count;        /* [1] free pages after the step; may be free_count_dev itself                  */
+    int32_t *cu_tokens;         /* [batch + 1] offsets of the sequences' new tokens                             */
+    int32_t *positions;         /* [capacity_tokens] a token's position in its sequence; -1 behind the last one */
+    int32_t *slots;             /* [capacity_tokens] page * 64 + row; -1 behind the last one                    */
+    int32_t *units;             /* [capacity_units, 4] tokens that share a page, in order: first token, number, page,
+                                   first row; -1 behind the last unit.  16-byte aligned                        */
+    int32_t *num_units;         /* [1]                                                                          */
+    int32_t *starts;            /* [batch, 4] scratch, 16-byte aligned                                          */
+    int32_t *status;            /* [1] BF1_DEV_* bits; written by bf1_plan_cache, OR-ed by bf1_cache_write      */
+} bf1_cache_plan;               /* all pointers: device memory owned by the caller                              */
+
+/* Units that a step of `tokens` tokens in `batch` sequences may have.  Host only; -1 on bad arguments. */
+int32_t bf1_cache_plan_units(int32_t batch, int32_t tokens);
+
+/*   seqlens_dev     [batch] cached tokens before the step
+ *   new_lens_dev    [batch] tokens that the step adds; -1 releases the sequence
+ *   page_table_dev  [batch, max_pages_per_seq]: the entries of pages that hold tokens are read, those of fresh pages written; a
+ *                   released sequence's row stays as it is
+ *   free_pages_dev  [num_pages] a stack of free pages, free_count_dev [1] of them.  Released pages are put on it first, in the
+ *                   order of sequences and blocks, then fresh ones are taken from its top in that order.  Both NULL: the table
+ *                   names all pages already, and releasing a sequence only sets its length to 0
+ * A step is refused as a whole where it cannot be carried out: BF1_DEV_BAD_SEQLENS (a negative length, new_lens below -1, more
+ * pages than max_pages_per_seq), BF1_DEV_CAPACITY (more tokens than capacity_tokens, too few free pages, more free pages than
+ * num_pages).  Lengths, free pages and table are then as they were, and there are no tokens and no units.  A page that the table
+ * or the stack names outside [0, num_pages) sets BF1_DEV_BAD_ROUTE, and its tokens have slot -1.  Nothing finds out that a page
+ * is named twice.  Arrays other than the two named above must not overlap. */
+int bf1_plan_cache(const int32_t *seqlens_dev, const int32_t *new_lens_dev, int32_t *page_table_dev, int32_t max_pages_per_seq,
+                   int32_t num_pages, int32_t *free_pages_dev, const int32_t *free_count_dev,
+                   const bf1_cache_plan *out /* host struct, device arrays */, void *stream);
+
+/* Puts the keys and values of the plan's tokens into the pages, [num_pages, 64, hkv, d].
+ *   k, v      rows of heads, `tokens` = the plan's capacity_tokens; rows behind the last token are not read
+ *   k_scales, v_scales   both NULL: the pages are bf16.  Otherwise they are 8-bit numbers (e4m3: 4 exponent bits, 3 of fraction,
+ *             largest 448) under fp32 scales [num_pages, hkv], value = number * scale.  A page and head's scale is the smallest
+ *             power of two, at least 2^-64, that holds all finite values of its rows; where a later token needs a larger one, the
+ *             rows in front of it are moved under that (which rounds only what is below 2^-6 of the new scale), and one that is
+ *             larger already stays until the page is begun anew from row 0.  Infinities and NaN are stored as NaN.
+ *   rope      not NULL: keys are rotated to the plan's positions on their way, rounded once, to what the page holds
+ *   q, out_q  with a rope: hq query heads that are rotated too, by the same call (hq = 0: none; not read).  Rows of padding are
+ *             not written.  out_q may be q
+ * Other rows of a page are left as they are.  Two sequences that write to one page in the same step race for its scale.  A unit that does
+ * not fit the tensors sets BF1_DEV_BAD_ROUTE and is left out. */
+int bf1_cache_write(const bf1_rows *k, const bf1_rows *v, const bf1_rows *q, int32_t tokens, int32_t hq, int32_t hkv, int32_t d,
+                    const bf1_cache_plan *plan /* host */, const bf1_rope *rope /* host */, int32_t num_pages, void *k_pages,
+                    void *v_pages, float *k_scales, float *v_scales, const bf1_rows *out_q, void *stream);
+
 /* Message for the last non-OK status returned on the calling thread ("" if none). */
 const char *bf1_last_error(void);
 

@@ -27,6 +27,7 @@ EXPORTS = ("bf1_route_capacity", "bf1_plan_route", "bf1_attn_fwd", "bf1_dense_ca
            "bf1_attn_bwd", "bf1_attn_bwd_workspace_bytes", "bf1_shard_needed_blocks", "bf1_plan_route_shard",
            "bf1_shard_needed_blocks_strided", "bf1_plan_route_shard_strided",
            "bf1_rope_turns", "bf1_rope_fwd", "bf1_rope_bwd",
+           "bf1_cache_plan_units", "bf1_plan_cache", "bf1_cache_write",
            "bf1_last_error", "bf1_version")
 
 
@@ -69,6 +70,14 @@ class _RopeC(ctypes.Structure):
 class _RowsC(ctypes.Structure):
     """Mirror of bf1_rows."""
     _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class _CachePlanC(ctypes.Structure):
+    """Mirror of bf1_cache_plan."""
+    _fields_ = [("batch", ctypes.c_int32), ("capacity_tokens", ctypes.c_int32), ("capacity_units", ctypes.c_int32),
+                ("seqlens", ctypes.c_void_p), ("free_count", ctypes.c_void_p), ("cu_tokens", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("slots", ctypes.c_void_p), ("units", ctypes.c_void_p), ("num_units", ctypes.c_void_p), ("starts", ctypes.c_void_p),
+                ("status", ctypes.c_void_p)]
 
 
 class Bf1Error(RuntimeError):
@@ -127,6 +136,13 @@ def load():
     for name in ("bf1_rope_fwd", "bf1_rope_bwd"):
         getattr(L, name).restype = ctypes.c_int
         getattr(L, name).argtypes = [rows, rows, vp, i32, i32, i32, i32, ropep, rows, rows, vp]
+    cache = ctypes.POINTER(_CachePlanC)
+    L.bf1_cache_plan_units.restype = i32
+    L.bf1_cache_plan_units.argtypes = [i32, i32]
+    L.bf1_plan_cache.restype = ctypes.c_int
+    L.bf1_plan_cache.argtypes = [vp, vp, vp, i32, i32, vp, vp, cache, vp]
+    L.bf1_cache_write.restype = ctypes.c_int
+    L.bf1_cache_write.argtypes = [rows, rows, rows, i32, i32, i32, i32, cache, ropep, i32, vp, vp, vp, vp, rows, vp]
     L.bf1_last_error.restype = ctypes.c_char_p
     L.bf1_last_error.argtypes = []
     L.bf1_version.restype = ctypes.c_int
@@ -401,6 +417,74 @@ def rope_fwd(q, k, positions, rope: Rope, out_q=None, out_k=None, stream=None):
 def rope_bwd(d_q, d_k, positions, rope: Rope, out_q=None, out_k=None, stream=None):
     """bf1_rope_bwd: the gradients of q and k before the rotation, from those behind it.  Arguments as rope_fwd."""
     return _host().rope(1, d_q, d_k, positions, ctypes.addressof(rope.c), rope.turns, out_q, out_k, _stream_ptr(stream))
+
+
+@dataclass
+class CachePlan:
+    """Device arrays of a serving step's tables plus the C struct: where the step's tokens stand in their sequences and in the pages."""
+    batch: int
+    tokens: int
+    seqlens: torch.Tensor
+    free_count: torch.Tensor
+    cu_tokens: torch.Tensor
+    positions: torch.Tensor
+    slots: torch.Tensor
+    units: torch.Tensor
+    num_units: torch.Tensor
+    starts: torch.Tensor
+    status: torch.Tensor
+    c: _CachePlanC = None
+
+    @staticmethod
+    def empty(batch: int, tokens: int, device) -> "CachePlan":
+        """Arrays for steps of up to `tokens` tokens in `batch` sequences."""
+        units = int(load().bf1_cache_plan_units(batch, tokens))
+        if units < 0:
+            raise ValueError("batch and tokens must not be negative")
+        i32 = dict(dtype=torch.int32, device=device)
+        p = CachePlan(batch, tokens, torch.zeros(batch, **i32), torch.zeros(1, **i32), torch.zeros(batch + 1, **i32),
+                      torch.full((tokens,), -1, **i32), torch.full((tokens,), -1, **i32), torch.full((units, 4), -1, **i32),
+                      torch.zeros(1, **i32), torch.zeros((max(batch, 1), 4), **i32), torch.zeros(1, **i32))
+        some = p.status.data_ptr()     # (an array without entries has no address)
+        at = lambda t: t.data_ptr() or some  # noqa: E731
+        p.c = _CachePlanC(batch, tokens, units, at(p.seqlens), at(p.free_count), at(p.cu_tokens), at(p.positions), at(p.slots), at(p.units),
+                          at(p.num_units), at(p.starts), at(p.status))
+        return p
+
+    def check_status(self):
+        """Synchronising read of the device status word; raises if any BF1_DEV_* bit is set."""
+        st = int(self.status.item())
+        if st:
+            raise Bf1Error(-100, "device status 0x%x" % st)
+
+
+def plan_cache(seqlens: torch.Tensor, new_lens: torch.Tensor, page_table: torch.Tensor, num_pages: int, tokens: int, free_pages=None,
+               free_count=None, plan: Optional[CachePlan] = None, seqlens_out=None, free_count_out=None, stream=None) -> CachePlan:
+    """bf1_plan_cache: the tables of a step that adds new_lens[s] tokens (-1: releases the sequence) to seqlens[s] cached ones.
+
+    page_table [batch, pages] is completed with pages from the stack free_pages [num_pages], of which free_count are there (without
+    them it has to be complete).  `tokens`: rows of the step's packed tensors, at least the tokens it adds.  The lengths and the number
+    of free pages after the step are in plan.seqlens and plan.free_count, or in seqlens_out / free_count_out, which may be the
+    inputs themselves."""
+    if plan is None:
+        plan = CachePlan.empty(seqlens.numel(), tokens, seqlens.device)
+    elif plan.tokens != tokens:
+        raise ValueError("the plan is for %d tokens, not %d" % (plan.tokens, tokens))
+    _host().plan_cache(seqlens, new_lens, page_table, num_pages, free_pages, free_count, ctypes.addressof(plan.c), plan.status,
+                       plan.seqlens if seqlens_out is None else seqlens_out, plan.free_count if free_count_out is None else free_count_out,
+                       _stream_ptr(stream))
+    return plan
+
+
+def cache_write(k, v, k_pages, v_pages, plan: CachePlan, k_scales=None, v_scales=None, rope: Optional[Rope] = None, q=None, out_q=None,
+                stream=None):
+    """bf1_cache_write: a step's keys and values [plan.tokens, hkv, d] bf16 (rows and heads may be strided) into the pages.
+
+    k_pages / v_pages [pages, 64, hkv, d]: bf16, or float8_e4m3fn with k_scales / v_scales [pages, hkv] fp32.  With `rope` the keys are
+    rotated to plan.positions on their way, and so are the queries q, into out_q (made if None), which is returned."""
+    return _host().cache_write(k, v, k_pages, v_pages, ctypes.addressof(plan.c), plan.status, k_scales, v_scales,
+                               None if rope is None else ctypes.addressof(rope.c), None if rope is None else rope.turns, q, out_q,
+                               _stream_ptr(stream))
 
 
 def shard_needed_blocks(n_tokens: int, lo_block: int, hi_block: int, cfg: Optional[RouteCfg] = None):

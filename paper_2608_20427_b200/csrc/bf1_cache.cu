@@ -1,0 +1,530 @@
+// The paged cache: the tables of a serving step, and its keys and values put into the pages.
+//
+// plan_cache_kernel turns lengths into everything that the step's other calls look up: pages taken from a stack of free ones and
+// written into the page table, where each new token stands (position, slot), and the runs of tokens that share a page (units).
+// One thread-block cluster does it: every CTA reads all lengths and scans them by itself, so nothing is exchanged; the
+// cluster's barrier stands between the reads of arrays that may be written in place and their writes.
+//
+// The write kernels go by units.  In 8 bits the rows of a page and KV head share a scale, so whoever writes to a page has to see all of the
+// step's rows for it: a unit is what one CTA (or half a warp) does.  Scales are powers of two: e4m3 has the same precision in every
+// binade, so that a finer scale would gain nothing, and rows that have to move under a larger scale keep their digits (but for
+// those that fall below 2^-6 of it, which have fewer at any scale).
+#include <math.h>
+
+#include <algorithm>
+#include <atomic>
+#include <cfloat>
+
+#include "bf1_rope.cuh"
+
+namespace bf1 {
+
+constexpr int kCachePage = 64;
+constexpr int kTableThreads = 1024;
+constexpr int kTableWarps = kTableThreads / 32;
+
+struct TableArgs {
+    const int32_t *lens, *add;         // [batch]
+    int32_t* table;                    // [batch, max_pages]
+    int32_t* free_pages;               // stack of free pages, or null: the table is complete
+    const int32_t* free_count;
+    int32_t batch, max_pages, num_pages;
+    bf1_cache_plan p;
+};
+
+__device__ __forceinline__ int pages_of(int n) { return (n + kCachePage - 1) / kCachePage; }
+
+// Exclusive prefix sums over the CTA of four numbers of every thread at once; `total` gets the sums.  Two barriers.
+__device__ __forceinline__ int4 scan4(int4 v, int4* warp_sums, int4& total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int4 x = v;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const int a = __shfl_up_sync(0xffffffffu, x.x, off), b = __shfl_up_sync(0xffffffffu, x.y, off),
+                  c = __shfl_up_sync(0xffffffffu, x.z, off), d = __shfl_up_sync(0xffffffffu, x.w, off);
+        if (lane >= off) x.x += a, x.y += b, x.z += c, x.w += d;
+    }
+    __syncthreads();                                     // the last use of warp_sums is over
+    if (lane == 31) warp_sums[warp] = x;
+    __syncthreads();
+    int4 before = make_int4(0, 0, 0, 0);
+    total = before;
+    for (int w = 0; w < kTableWarps; ++w) {
+        const int4 s = warp_sums[w];
+        if (w < warp) before.x += s.x, before.y += s.y, before.z += s.z, before.w += s.w;
+        total.x += s.x, total.y += s.y, total.z += s.z, total.w += s.w;
+    }
+    return make_int4(before.x + x.x - v.x, before.y + x.y - v.y, before.z + x.z - v.z, before.w + x.w - v.w);
+}
+
+__global__ void __launch_bounds__(kTableThreads, 1) plan_cache_kernel(const TableArgs a) {
+    __shared__ int4 warp_sums[kTableWarps];
+    __shared__ long long sums[3];
+    __shared__ int flags;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int rank = blockIdx.x, ranks = gridDim.x;      // the grid is one cluster
+    const int threads = ranks * kTableThreads, gtid = rank * kTableThreads + tid;
+    const bool stack = a.free_pages != nullptr;
+    const bf1_cache_plan& p = a.p;
+    if (tid < 3) sums[tid] = 0;
+    if (tid == 0) flags = 0;
+    pdl_wait();
+    __syncthreads();
+    // ---- what the step needs in all, in 64 bits: it may be refused for any lengths ----------------------------------------------
+    long long tokens = 0, fresh = 0, back = 0;
+    int bad = 0;
+    for (int s = tid; s < a.batch; s += kTableThreads) {
+        const int n = a.lens[s], m = a.add[s];
+        if (n < 0 || m < -1 || (long long)n + max(m, 0) > (long long)a.max_pages * kCachePage) {
+            bad = BF1_DEV_BAD_SEQLENS;
+            continue;
+        }
+        tokens += max(m, 0);
+        if (stack) {
+            if (m < 0) back += pages_of(n);
+            else fresh += pages_of(n + m) - pages_of(n);
+        }
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) {
+        tokens += __shfl_xor_sync(0xffffffffu, tokens, off);
+        fresh += __shfl_xor_sync(0xffffffffu, fresh, off);
+        back += __shfl_xor_sync(0xffffffffu, back, off);
+        bad |= __shfl_xor_sync(0xffffffffu, bad, off);
+    }
+    if (lane == 0) {
+        atomicAdd(reinterpret_cast<unsigned long long*>(&sums[0]), (unsigned long long)tokens);
+        atomicAdd(reinterpret_cast<unsigned long long*>(&sums[1]), (unsigned long long)fresh);
+        atomicAdd(reinterpret_cast<unsigned long long*>(&sums[2]), (unsigned long long)back);
+        if (bad) atomicOr(&flags, bad);
+    }
+    __syncthreads();
+    const int had = stack ? *a.free_count : 0;
+    int status = flags;
+    if (sums[0] > p.capacity_tokens) status |= BF1_DEV_CAPACITY;
+    if (stack && (had < 0 || had + sums[2] > a.num_pages || sums[1] > had + sums[2])) status |= BF1_DEV_CAPACITY;
+    const bool refused = status != 0;
+    const int top = refused ? had : had + (int)sums[2];   // of the stack, with what is put back
+    const int total_tokens = refused ? 0 : (int)sums[0];
+    // ---- where every sequence's tokens, pages and units begin --------------------------------------------------------------------
+    int4 at = make_int4(0, 0, 0, 0);                      // tokens, fresh pages, units, pages put back
+    for (int s0 = 0; s0 < a.batch; s0 += kTableThreads) {
+        const int s = s0 + tid;
+        int n = 0, m = 0;
+        int4 mine = make_int4(0, 0, 0, 0);
+        if (s < a.batch && !refused) {
+            n = a.lens[s];
+            m = a.add[s];
+            mine.x = max(m, 0);
+            mine.y = stack && m > 0 ? pages_of(n + m) - pages_of(n) : 0;
+            mine.z = m > 0 ? (n + m - 1) / kCachePage - n / kCachePage + 1 : 0;
+            mine.w = stack && m < 0 ? pages_of(n) : 0;
+        } else if (s < a.batch) {
+            n = a.lens[s];
+        }
+        int4 total;
+        const int4 before = scan4(mine, warp_sums, total);
+        if (s < a.batch && s0 / kTableThreads % ranks == rank) {
+            p.cu_tokens[s] = at.x + before.x;
+            // a released sequence takes no pages: where its own go on the stack stands there instead
+            reinterpret_cast<int4*>(p.starts)[s] = make_int4(at.x + before.x, m < 0 ? at.w + before.w : at.y + before.y, at.z + before.z, n);
+        }
+        at.x += total.x, at.y += total.y, at.z += total.z, at.w += total.w;
+    }
+    if (gtid == 0) {
+        p.cu_tokens[a.batch] = at.x;
+        *p.num_units = at.z;
+        *p.status = status;
+    }
+    const int units = at.z;
+    cluster_arrive();
+    cluster_wait();                                       // lengths and the count have been read, the starts are there
+    if (gtid == 0) *p.free_count = top - at.y;
+    // ---- lengths after the step; pages put back ------------------------------------------------------------------------------------
+    const int4* starts = reinterpret_cast<const int4*>(p.starts);
+    for (int s0 = (rank * kTableWarps + warp) * 32; s0 < a.batch; s0 += threads) {
+        const int s = s0 + lane;
+        int m = 0, n = 0, to = 0;
+        if (s < a.batch) {
+            const int4 st = starts[s];
+            m = refused ? 0 : a.add[s];
+            n = st.w;
+            to = st.y;
+            p.seqlens[s] = m < 0 ? 0 : n + m;
+        }
+        unsigned gone = __ballot_sync(0xffffffffu, m < 0 && stack);
+        while (gone) {
+            const int l = __ffs(gone) - 1;
+            gone &= gone - 1;
+            const int count = pages_of(__shfl_sync(0xffffffffu, n, l)), first = had + __shfl_sync(0xffffffffu, to, l);
+            for (int i = lane; i < count; i += 32) a.free_pages[first + i] = a.table[(size_t)(s0 + l) * a.max_pages + i];
+        }
+    }
+    if (at.w > 0) {                                       // (the same in every CTA)
+        cluster_arrive();
+        cluster_wait();
+    }
+    // ---- fresh pages into the table ------------------------------------------------------------------------------------------------
+    if (at.y > 0) {
+        for (int s0 = (rank * kTableWarps + warp) * 32; s0 < a.batch; s0 += threads) {
+            const int s = s0 + lane;
+            int held = 0, want = 0, first = 0;
+            if (s < a.batch) {
+                const int4 st = starts[s];
+                const int m = a.add[s];
+                held = pages_of(st.w);
+                want = m > 0 ? pages_of(st.w + m) - held : 0;
+                first = st.y;
+            }
+            unsigned grown = __ballot_sync(0xffffffffu, want > 0);
+            while (grown) {
+                const int l = __ffs(grown) - 1;
+                grown &= grown - 1;
+                const int count = __shfl_sync(0xffffffffu, want, l), h = __shfl_sync(0xffffffffu, held, l), f = __shfl_sync(0xffffffffu, first, l);
+                for (int i = lane; i < count; i += 32) a.table[(size_t)(s0 + l) * a.max_pages + h + i] = a.free_pages[top - 1 - (f + i)];
+            }
+        }
+    }
+    // ---- positions, slots and units, four tokens to a thread -------------------------------------------------------------------------
+    for (int t0 = gtid * 4; t0 < p.capacity_tokens; t0 += threads * 4) {
+        int s = 0;
+        int4 st = make_int4(0, 0, 0, 0);
+        int end = 0;
+        if (t0 < total_tokens) {                          // the last sequence that begins at or in front of t0
+            int lo = 0, hi = a.batch;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (starts[mid].x <= t0) lo = mid;
+                else hi = mid;
+            }
+            s = lo;
+            st = starts[s];
+            end = s + 1 < a.batch ? starts[s + 1].x : total_tokens;
+        }
+        for (int i = 0; i < 4 && t0 + i < p.capacity_tokens; ++i) {
+            const int t = t0 + i;
+            int pos = -1, slot = -1;
+            if (t < total_tokens) {
+                while (t >= end) {                        // (every token below the total belongs to some sequence)
+                    ++s;
+                    st = starts[s];
+                    end = s + 1 < a.batch ? starts[s + 1].x : total_tokens;
+                }
+                pos = st.w + (t - st.x);
+                const int lp = pos / kCachePage, row = pos % kCachePage, held = pages_of(st.w);
+                int page = stack && lp >= held ? a.free_pages[top - 1 - (st.y + lp - held)] : a.table[(size_t)s * a.max_pages + lp];
+                if (page < 0 || page >= a.num_pages) {
+                    atomicOr(p.status, BF1_DEV_BAD_ROUTE);
+                    page = -1;
+                } else {
+                    slot = page * kCachePage + row;
+                }
+                if (t == st.x || row == 0) {              // the first token of a unit
+                    const int u = st.z + lp - st.w / kCachePage;
+                    if (u < p.capacity_units) reinterpret_cast<int4*>(p.units)[u] = make_int4(t, min(kCachePage - row, end - t), page, row);
+                }
+            }
+            p.positions[t] = pos;
+            p.slots[t] = slot;
+        }
+    }
+    for (int u = units + gtid; u < p.capacity_units; u += threads) reinterpret_cast<int4*>(p.units)[u] = make_int4(-1, -1, -1, -1);
+}
+
+
+// ---- keys and values into the pages ------------------------------------------------------------------------------------------------
+
+struct WriteArgs {
+    Rows x[2];                         // keys, values
+    Rows q, out_q;
+    uint8_t* pages[2];                 // [num_pages, 64, hkv, D], bf16 or e4m3
+    float* scales[2];                  // [num_pages, hkv] (8 bits)
+    const int4* units;
+    const int32_t *num_units, *positions;
+    int32_t* status;
+    RopeTable rope;                    // dim 0: nothing is rotated
+    int32_t tokens, hq, hkv, num_pages, capacity_units;
+    int64_t write_ctas;                // CTAs behind them rotate queries
+    int32_t q_shares;                  // shares of the query heads
+};
+
+__device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
+    uint16_t lo, hi;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
+    return lo | (uint32_t)hi << 16;
+}
+__device__ __forceinline__ float2 from_e4m3x2(uint32_t v) {
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)v));
+    float2 f;
+    asm("{\n\t.reg .f16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.f32.f16 %0, a;\n\tcvt.f32.f16 %1, b;\n\t}" : "=f"(f.x), "=f"(f.y) : "r"(h));
+    return f;
+}
+// Largest magnitude that counts for a scale (an infinity and a NaN do not: they are stored as NaN under any)
+__device__ __forceinline__ float magnitude_of(const float (&x)[8], float top) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float m = fabsf(x[i]);
+        if (m <= FLT_MAX) top = fmaxf(top, m);
+    }
+    return top;
+}
+// The smallest power of two, 2^-64 at least, under which `top` is within 448 = 1.75 * 2^8.
+__device__ __forceinline__ float scale_for(float top) {
+    const int e = (int)((__float_as_uint(top) + 0x1fffffu) >> 23) - 8;     // above 1.75 the sum carries into the exponent
+    return __uint_as_float((uint32_t)max(e, 127 - 64) << 23);
+}
+__device__ __forceinline__ uint2 quantize(const float (&x)[8], float inv) {   // inv: a power of two, so that the product is exact
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = fabsf(x[i]) <= FLT_MAX ? x[i] * inv : NAN;
+    return make_uint2(e4m3x4(y[0], y[1], y[2], y[3]), e4m3x4(y[4], y[5], y[6], y[7]));
+}
+__device__ __forceinline__ uint2 requantize(uint2 v, float ratio) {
+    const float2 a = from_e4m3x2(v.x & 0xffffu), b = from_e4m3x2(v.x >> 16), c = from_e4m3x2(v.y & 0xffffu), d = from_e4m3x2(v.y >> 16);
+    return make_uint2(e4m3x4(a.x * ratio, a.y * ratio, b.x * ratio, b.y * ratio), e4m3x4(c.x * ratio, c.y * ratio, d.x * ratio, d.y * ratio));
+}
+
+// A unit whose tokens, rows and page exist.  What a plan holds is looked at once more here: a plan for other tensors than these, or one
+// that has been written over, costs the unit and not memory.
+__device__ __forceinline__ bool unit_ok(const WriteArgs& a, const int4& u) {
+    return u.x >= 0 && u.y >= 1 && u.y <= a.tokens - u.x && u.w >= 0 && u.w + u.y <= kCachePage && u.z >= 0 && u.z < a.num_pages;
+}
+
+// The CTAs behind the writing ones: tokens' queries, as rope_kernel does them.
+template <int D>
+__device__ __forceinline__ void rotate_queries(const WriteArgs& a) {
+    constexpr int kPerToken = D / 16, kTokens = 128 / kPerToken;
+    const int64_t block = (int64_t)blockIdx.x - a.write_ctas;
+    const int64_t token = block / a.q_shares * kTokens + threadIdx.x / kPerToken;
+    if (token >= a.tokens) return;
+    const int position = a.positions[token];
+    if (position < 0) return;
+    rope_heads<4>(a.rope, position, token, threadIdx.x % kPerToken, 1.f, a.q, a.q, a.out_q, a.out_q, a.hq, a.hq, (int)(block % a.q_shares), a.q_shares);
+}
+
+// A CTA per unit, KV head and K or V: the rows stay in registers between the look for their largest value and the store.
+template <int D, bool kFp8>
+__global__ void __launch_bounds__(128) cache_write_pages_kernel(const WriteArgs a) {
+    constexpr int kChunks = D / 8, kRows = 128 / kChunks, kPer = kCachePage / kRows;
+    __shared__ float warp_top[4];
+    pdl_wait();
+    if ((int64_t)blockIdx.x >= a.write_ctas) return rotate_queries<D>(a);
+    const int which = blockIdx.x & 1, h = (blockIdx.x >> 1) % a.hkv, unit = (blockIdx.x >> 1) / a.hkv;
+    if (unit >= *a.num_units) return;
+    const int4 u = a.units[unit];
+    if (!unit_ok(a, u)) {
+        if (threadIdx.x == 0) atomicOr(a.status, BF1_DEV_BAD_ROUTE);
+        return;
+    }
+    const int c = threadIdx.x % kChunks, r0 = threadIdx.x / kChunks;
+    const Rows& in = a.x[which];
+    float x[kPer][8], top = 0.f;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int r = r0 + i * kRows;
+        if (r < u.y) {
+            const __nv_bfloat16* row = in.at((int64_t)u.x + r, h);
+            if (which == 0 && a.rope.dim) rope_chunk(a.rope, a.positions[u.x + r], row, c, x[i]);
+            else unpack_bf16x8(*reinterpret_cast<const uint4*>(row + 8 * c), x[i]);
+            top = magnitude_of(x[i], top);
+        }
+    }
+    const size_t pitch = (size_t)a.hkv * D;
+    const size_t first = ((size_t)u.z * kCachePage) * pitch + (size_t)h * D + 8 * c;     // element of the page's row 0
+    if constexpr (!kFp8) {
+        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.pages[which]) + first;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int r = r0 + i * kRows;
+            if (r < u.y) *reinterpret_cast<uint4*>(out + (u.w + r) * pitch) = pack_bf16x8(x[i]);
+        }
+        return;
+    }
+    float* const at = a.scales[which] + (size_t)u.z * a.hkv + h;
+    const float before = u.w > 0 ? *at : 0.f;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+    if ((threadIdx.x & 31) == 0) warp_top[threadIdx.x >> 5] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(warp_top[0], warp_top[1]), fmaxf(warp_top[2], warp_top[3]));
+    const float scale = fmaxf(scale_for(top), before), inv = 1.f / scale;
+    uint8_t* out = a.pages[which] + first;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int r = r0 + i * kRows;
+        if (r < u.y) *reinterpret_cast<uint2*>(out + (u.w + r) * pitch) = quantize(x[i], inv);
+    }
+    if (u.w > 0 && before != scale)
+        for (int r = r0; r < u.w; r += kRows) {
+            uint2* v = reinterpret_cast<uint2*>(out + r * pitch);
+            *v = requantize(*v, before * inv);
+        }
+    if (threadIdx.x == 0) *at = scale;
+}
+
+// A warp per unit and KV head, half of it for K and half for V: for units of a token or a few, which a CTA would not fill.
+template <int D, bool kFp8>
+__global__ void __launch_bounds__(128) cache_write_tokens_kernel(const WriteArgs a) {
+    constexpr int kChunks = D / 8, kRows = 16 / kChunks;        // lanes to a row, rows at a time
+    pdl_wait();
+    if ((int64_t)blockIdx.x >= a.write_ctas) return rotate_queries<D>(a);
+    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+    const int unit = (int)(item / a.hkv), h = (int)(item % a.hkv);
+    if (unit >= min(*a.num_units, a.capacity_units)) return;    // (the last CTA may have warps to spare)
+    const int4 u = a.units[unit];
+    const int lane = threadIdx.x & 31, which = lane >> 4, c = lane % kChunks, r0 = (lane & 15) / kChunks;
+    if (!unit_ok(a, u)) {
+        if (lane == 0) atomicOr(a.status, BF1_DEV_BAD_ROUTE);
+        return;
+    }
+    const Rows& in = a.x[which];
+    auto load = [&](int r, float (&x)[8]) {
+        const __nv_bfloat16* row = in.at((int64_t)u.x + r, h);
+        if (which == 0 && a.rope.dim) rope_chunk(a.rope, a.positions[u.x + r], row, c, x);
+        else unpack_bf16x8(*reinterpret_cast<const uint4*>(row + 8 * c), x);
+    };
+    const size_t pitch = (size_t)a.hkv * D;
+    const size_t first = ((size_t)u.z * kCachePage) * pitch + (size_t)h * D + 8 * c;
+    float x[8];
+    if constexpr (!kFp8) {
+        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.pages[which]) + first;
+        for (int r = r0; r < u.y; r += kRows) {
+            load(r, x);
+            *reinterpret_cast<uint4*>(out + (u.w + r) * pitch) = pack_bf16x8(x);
+        }
+        return;
+    }
+    float* const at = a.scales[which] + (size_t)u.z * a.hkv + h;
+    const float before = u.w > 0 ? *at : 0.f;
+    float top = 0.f;
+    for (int r = r0 + (u.y - 1) / kRows * kRows; r >= 0; r -= kRows)       // the first rows last: they stay in x
+        if (r < u.y) {
+            load(r, x);
+            top = magnitude_of(x, top);
+        }
+#pragma unroll
+    for (int off = 8; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+    const float scale = fmaxf(scale_for(top), before), inv = 1.f / scale;
+    uint8_t* out = a.pages[which] + first;
+    for (int r = r0; r < u.y; r += kRows) {
+        if (r != r0) load(r, x);
+        *reinterpret_cast<uint2*>(out + (u.w + r) * pitch) = quantize(x, inv);
+    }
+    if (u.w > 0 && before != scale) {
+        constexpr int kAhead = 8;
+        for (int r = r0; r < u.w; r += kAhead * kRows) {
+            uint2 v[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (r + i * kRows < u.w) v[i] = *reinterpret_cast<const uint2*>(out + (r + i * kRows) * pitch);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (r + i * kRows < u.w) *reinterpret_cast<uint2*>(out + (r + i * kRows) * pitch) = requantize(v[i], before * inv);
+        }
+    }
+    if ((lane & 15) == 0) *at = scale;
+}
+
+typedef void (*WriteKernel)(WriteArgs);
+
+static int check_plan(const bf1_cache_plan* p) {
+    if (!p) return fail(BF1_ERR_INVALID_ARG, "the cache plan is null");
+    if (p->batch < 0 || p->batch > 65535 || p->capacity_tokens < 0 || p->capacity_tokens > (1 << 30) || p->capacity_units < 0)
+        return fail(BF1_ERR_INVALID_ARG, "cache plan: batch, capacity_tokens or capacity_units out of range");
+    if (!p->seqlens || !p->free_count || !p->cu_tokens || !p->positions || !p->slots || !p->units || !p->num_units || !p->starts || !p->status)
+        return fail(BF1_ERR_INVALID_ARG, "a cache-plan pointer is null");
+    if (((uintptr_t)p->units | (uintptr_t)p->starts) & 15) return fail(BF1_ERR_INVALID_ARG, "units and starts must be 16-byte aligned");
+    return BF1_OK;
+}
+
+}  // namespace bf1
+
+using namespace bf1;
+
+extern "C" int32_t bf1_cache_plan_units(int32_t batch, int32_t tokens) {
+    if (batch < 0 || tokens < 0) return -1;
+    const int64_t most = (int64_t)tokens / kCachePage + 2 * (int64_t)batch;   // n tokens touch at most (n + 62) / 64 + 1 pages
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>(tokens, most));
+}
+
+extern "C" int bf1_plan_cache(const int32_t* seqlens_dev, const int32_t* new_lens_dev, int32_t* page_table_dev, int32_t max_pages_per_seq,
+                              int32_t num_pages, int32_t* free_pages_dev, const int32_t* free_count_dev, const bf1_cache_plan* out,
+                              void* stream) {
+    if (int rc = check_plan(out)) return rc;
+    if (out->batch > 0 && (!seqlens_dev || !new_lens_dev || !page_table_dev)) return fail(BF1_ERR_INVALID_ARG, "seqlens, new_lens or page_table is null");
+    if ((free_pages_dev == nullptr) != (free_count_dev == nullptr)) return fail(BF1_ERR_INVALID_ARG, "free_pages and free_count go together");
+    if (max_pages_per_seq < 1 || max_pages_per_seq > (1 << 24) || num_pages < 1 || num_pages > (1 << 25) - 1)
+        return fail(BF1_ERR_UNSUPPORTED, "max_pages_per_seq up to 2^24 and num_pages up to 2^25 - 1");
+    const int need = bf1_cache_plan_units(out->batch, out->capacity_tokens);
+    if (out->capacity_units < need) return fail(BF1_ERR_CAPACITY, "cache plan capacity_units %d < %d", out->capacity_units, need);
+    TableArgs a;
+    a.lens = seqlens_dev;
+    a.add = new_lens_dev;
+    a.table = page_table_dev;
+    a.free_pages = free_pages_dev;
+    a.free_count = free_count_dev;
+    a.batch = out->batch;
+    a.max_pages = max_pages_per_seq;
+    a.num_pages = num_pages;
+    a.p = *out;
+    const int ctas = out->capacity_tokens <= 4096 ? 1 : 8;
+    BF1_CUDA_CHECK(launch_pdl_cluster(plan_cache_kernel, dim3(ctas), dim3(ctas), kTableThreads, 0, (cudaStream_t)stream, a));
+    return BF1_OK;
+}
+
+extern "C" int bf1_cache_write(const bf1_rows* k, const bf1_rows* v, const bf1_rows* q, int32_t tokens, int32_t hq, int32_t hkv, int32_t d,
+                               const bf1_cache_plan* plan, const bf1_rope* rope, int32_t num_pages, void* k_pages, void* v_pages,
+                               float* k_scales, float* v_scales, const bf1_rows* out_q, void* stream) {
+    if (int rc = check_plan(plan)) return rc;
+    if (tokens < 0 || hkv < 1 || hq < 0 || num_pages < 1) return fail(BF1_ERR_INVALID_ARG, "bad token, head or page count");
+    if (d != 64 && d != 128) return fail(BF1_ERR_UNSUPPORTED, "head dimension %d: only 64 and 128 are supported", d);
+    if (tokens != plan->capacity_tokens) return fail(BF1_ERR_INVALID_ARG, "%d tokens, the plan is for %d", tokens, plan->capacity_tokens);
+    if (hkv > 65535 || hq > 65535) return fail(BF1_ERR_UNSUPPORTED, "%d query and %d KV heads", hq, hkv);
+    if (!k_pages || !v_pages) return fail(BF1_ERR_INVALID_ARG, "k_pages or v_pages is null");
+    if (((uintptr_t)k_pages | (uintptr_t)v_pages) & 15) return fail(BF1_ERR_INVALID_ARG, "k_pages and v_pages must be 16-byte aligned");
+    if ((k_scales == nullptr) != (v_scales == nullptr)) return fail(BF1_ERR_INVALID_ARG, "k_scales and v_scales go together");
+    if (hq > 0 && !rope) return fail(BF1_ERR_INVALID_ARG, "queries are there to be rotated: no rope is given");
+    if (rope)
+        if (int rc = check_rope(rope, d)) return rc;
+    if (tokens == 0 || plan->batch == 0) return BF1_OK;
+    const bf1_rows* rows[4] = {k, v, q, out_q};
+    const char* const names[4] = {"k", "v", "q", "out_q"};
+    for (int i = 0; i < (hq ? 4 : 2); ++i)
+        if (int rc = check_rows(rows[i], names[i])) return rc;
+    if (hq && q->data == out_q->data && (q->row_stride != out_q->row_stride || q->head_stride != out_q->head_stride))
+        return fail(BF1_ERR_INVALID_ARG, "out_q in place of q has to have its strides");
+    WriteArgs a;
+    a.x[0] = rows_of(k);
+    a.x[1] = rows_of(v);
+    a.q = hq ? rows_of(q) : a.x[0];
+    a.out_q = hq ? rows_of(out_q) : a.x[0];
+    a.pages[0] = static_cast<uint8_t*>(k_pages);
+    a.pages[1] = static_cast<uint8_t*>(v_pages);
+    a.scales[0] = k_scales;
+    a.scales[1] = v_scales;
+    a.units = reinterpret_cast<const int4*>(plan->units);
+    a.num_units = plan->num_units;
+    a.positions = plan->positions;
+    a.status = plan->status;
+    a.rope = rope ? table_of(rope) : RopeTable{nullptr, 0, 0, 1.f};
+    a.tokens = tokens;
+    a.hq = hq;
+    a.hkv = hkv;
+    a.num_pages = num_pages;
+    a.capacity_units = plan->capacity_units;
+    static const WriteKernel kernels[2][2][2] = {   // [few tokens to a unit][8 bits][d = 128]
+        {{cache_write_pages_kernel<64, false>, cache_write_pages_kernel<128, false>}, {cache_write_pages_kernel<64, true>, cache_write_pages_kernel<128, true>}},
+        {{cache_write_tokens_kernel<64, false>, cache_write_tokens_kernel<128, false>}, {cache_write_tokens_kernel<64, true>, cache_write_tokens_kernel<128, true>}}};
+    const bool few = tokens < 8 * (int64_t)plan->batch;
+    const int64_t units = bf1_cache_plan_units(plan->batch, tokens);
+    if (plan->capacity_units < units) return fail(BF1_ERR_CAPACITY, "cache plan capacity_units %d < %d", plan->capacity_units, (int)units);
+    a.write_ctas = few ? (units * hkv + 3) / 4 : units * hkv * 2;
+    const int64_t token_ctas = ((int64_t)tokens + 128 / (d / 16) - 1) / (128 / (d / 16));
+    a.q_shares = hq ? (int)std::max<int64_t>(1, std::min<int64_t>(hq, 148 * 8 / token_ctas)) : 0;
+    const int64_t ctas = a.write_ctas + token_ctas * a.q_shares;
+    if (ctas > 0x7fffffffLL) return fail(BF1_ERR_UNSUPPORTED, "%d tokens of %d query and %d KV heads in one call", tokens, hq, hkv);
+    BF1_CUDA_CHECK(launch_pdl(kernels[few][k_scales != nullptr][d == 128], dim3((unsigned)ctas), 128, 0, (cudaStream_t)stream, a));
+    return BF1_OK;
+}

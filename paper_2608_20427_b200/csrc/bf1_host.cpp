@@ -266,6 +266,85 @@ PyObject* rope(PyObject* const* a) {
     return t;
 }
 
+// plan_cache(seqlens, new_lens, page_table, num_pages, free_pages*, free_count*, plan address, its status, seqlens_out, free_count_out, stream*)
+PyObject* plan_cache(PyObject* const* a) {
+    const at::Tensor &lens = tensor(a[0]), &add = tensor(a[1]), &table = tensor(a[2]);
+    const Place place(lens, a[10]);
+    const char* const what = "plan_cache: contiguous int32 tensors on one CUDA device";
+    const auto *lp = array_of<const int32_t>(lens, lens, at::kInt, what), *np = array_of<const int32_t>(add, lens, at::kInt, what);
+    auto* tp = array_of<int32_t>(table, lens, at::kInt, what);
+    array_of<int32_t>(tensor(a[7]), lens, at::kInt, "the plan must be on the device of the tensors");
+    bf1_cache_plan plan = *address<const bf1_cache_plan>(a[6]);
+    const long long num_pages = integer(a[3]);
+    require(num_pages >= 1 && num_pages <= INT32_MAX, "num_pages out of range");
+    require(lens.dim() == 1 && lens.size(0) == plan.batch && add.sizes() == lens.sizes() && table.dim() == 2 && table.size(0) == plan.batch,
+            "seqlens and new_lens must be [batch], page_table [batch, pages], batch the plan's");
+    require((a[4] == Py_None) == (a[5] == Py_None), "free_pages and free_count go together");
+    int32_t* fp = nullptr;
+    const int32_t* cp = nullptr;
+    if (a[4] != Py_None) {
+        const at::Tensor &pages = tensor(a[4]), &count = tensor(a[5]);
+        fp = array_of<int32_t>(pages, lens, at::kInt, what);
+        cp = array_of<const int32_t>(count, lens, at::kInt, what);
+        require(pages.numel() >= num_pages && count.numel() == 1, "free_pages must have room for num_pages, free_count must be one number");
+    }
+    const at::Tensor &lens_out = tensor(a[8]), &count_out = tensor(a[9]);
+    require(lens_out.sizes() == lens.sizes() && count_out.numel() == 1, "seqlens_out must be [batch], free_count_out one number");
+    if (plan.batch > 0) plan.seqlens = array_of<int32_t>(lens_out, lens, at::kInt, what);
+    plan.free_count = array_of<int32_t>(count_out, lens, at::kInt, what);
+    const int32_t width = static_cast<int32_t>(table.size(1));
+    call([&] { return bf1_plan_cache(lp, np, tp, width, static_cast<int32_t>(num_pages), fp, cp, &plan, place.stream); });
+    Py_RETURN_NONE;
+}
+
+// cache_write(k, v, k_pages, v_pages, plan address, its status, k_scales*, v_scales*, rope address*, its table*, q*, out_q*, stream*)
+PyObject* cache_write(PyObject* const* a) {
+    const at::Tensor &k = tensor(a[0]), &v = tensor(a[1]), &kp = tensor(a[2]), &vp = tensor(a[3]);
+    const Place place(k, a[12]);
+    const char* const what = "k, v, q and out_q must be 3-d bf16 tensors on one CUDA device, the last dimension contiguous";
+    const bf1_rows kr = rows_of(k, k, what), vr = rows_of(v, k, what);
+    require(v.sizes() == k.sizes(), "k and v must have the same shape");
+    const auto* plan = address<const bf1_cache_plan>(a[4]);
+    array_of<int32_t>(tensor(a[5]), k, at::kInt, "the plan must be on the device of the tensors");
+    const bool scaled = a[6] != Py_None;
+    require(scaled == (a[7] != Py_None), "k_scales and v_scales go together");
+    const at::ScalarType type = scaled ? at::kFloat8_e4m3fn : at::kBFloat16;
+    for (const at::Tensor* t : {&kp, &vp}) {
+        array_of<void>(*t, k, type, scaled ? "with scales the pages must be contiguous float8_e4m3fn tensors" : "without scales the pages must be contiguous bf16 tensors");
+        require(t->dim() == 4 && t->size(1) == 64 && t->size(2) == k.size(1) && t->size(3) == k.size(2) && t->size(0) == kp.size(0) && t->size(0) <= INT32_MAX,
+                "k_pages and v_pages must be [pages, 64, hkv, d]");
+    }
+    float* scales[2] = {nullptr, nullptr};
+    for (int i = 0; scaled && i < 2; ++i) {
+        const at::Tensor& t = tensor(a[6 + i]);
+        scales[i] = array_of<float>(t, k, at::kFloat, "k_scales and v_scales must be contiguous fp32 tensors");
+        require(t.dim() == 2 && t.size(0) == kp.size(0) && t.size(1) == k.size(1), "k_scales and v_scales must be [pages, hkv]");
+    }
+    const bf1_rope* rope = nullptr;
+    if (a[8] != Py_None) {
+        rope = address<const bf1_rope>(a[8]);
+        check_table(tensor(a[9]), k);
+    }
+    const bool queries = a[10] != Py_None;
+    bf1_rows qr = {}, oq = {};
+    at::Tensor out_q;
+    int32_t hq = 0;
+    if (queries) {
+        const at::Tensor& q = tensor(a[10]);
+        qr = rows_of(q, k, what);
+        require(q.size(0) == k.size(0) && q.size(2) == k.size(2), "q and k must have the same tokens and head dimension");
+        out_q = a[11] == Py_None ? at::empty(q.sizes(), q.options()) : tensor(a[11]);
+        require(out_q.sizes() == q.sizes(), "out_q must have the shape of q");
+        oq = rows_of(out_q, k, what);
+        hq = q.size(1);
+    }
+    const int32_t tokens = k.size(0), hkv = k.size(1), d = k.size(2), pages = kp.size(0);
+    void *kpp = kp.data_ptr(), *vpp = vp.data_ptr();
+    call([&] { return bf1_cache_write(&kr, &vr, &qr, tokens, hq, hkv, d, plan, rope, pages, kpp, vpp, scales[0], scales[1], &oq, place.stream); });
+    if (queries) return THPVariable_Wrap(out_q);
+    Py_RETURN_NONE;
+}
+
 // Argument count, C++ and torch exceptions.
 template <PyObject* (*F)(PyObject* const*), int kArgs>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -298,6 +377,8 @@ PyMethodDef g_methods[] = {
     BF1_ENTRY(plan_decode, 5),
     BF1_ENTRY(decode, 10),
     BF1_ENTRY(rope, 9),
+    BF1_ENTRY(plan_cache, 11),
+    BF1_ENTRY(cache_write, 13),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_host", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

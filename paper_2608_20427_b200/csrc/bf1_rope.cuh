@@ -37,6 +37,13 @@ __device__ __forceinline__ uint4 pack_bf16x8(const float (&x)[8]) {
     return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
 }
 
+// One pair turned.  The products are rounded in a stated order, so that every kernel gives the same bits.
+__device__ __forceinline__ void rope_turn(float& x, float& y, float c, float s) {
+    const float p = x, q = y;
+    x = __fmaf_rn(p, c, -__fmul_rn(q, s));
+    y = __fmaf_rn(p, s, __fmul_rn(q, c));
+}
+
 // Rows of heads in global memory: bf16, the dimensions of a head side by side, strides in elements.
 struct Rows {
     __nv_bfloat16* p;
@@ -82,19 +89,12 @@ __device__ __forceinline__ void rope_heads(const RopeTable& r, int position, int
                 unpack_bf16x8(b[u], x1);
                 if (r.half) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float p = x0[i], q = x1[i];
-                        x0[i] = p * cs[i] - q * sn[i];
-                        x1[i] = p * sn[i] + q * cs[i];
-                    }
+                    for (int i = 0; i < 8; ++i) rope_turn(x0[i], x1[i], cs[i], sn[i]);
                 } else {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float p = x0[2 * i], q = x0[2 * i + 1], s = x1[2 * i], t = x1[2 * i + 1];
-                        x0[2 * i] = p * cs[i] - q * sn[i];
-                        x0[2 * i + 1] = p * sn[i] + q * cs[i];
-                        x1[2 * i] = s * cs[4 + i] - t * sn[4 + i];
-                        x1[2 * i + 1] = s * sn[4 + i] + t * cs[4 + i];
+                        rope_turn(x0[2 * i], x0[2 * i + 1], cs[i], sn[i]);
+                        rope_turn(x1[2 * i], x1[2 * i + 1], cs[4 + i], sn[4 + i]);
                     }
                 }
                 a[u] = pack_bf16x8(x0);
@@ -102,6 +102,31 @@ __device__ __forceinline__ void rope_heads(const RopeTable& r, int position, int
             }
             *reinterpret_cast<uint4*>(y + lo) = a[u];
             *reinterpret_cast<uint4*>(y + hi) = b[u];
+        }
+    }
+}
+
+// Dimensions 8 c .. 8 c + 7 of a row, rotated.
+__device__ __forceinline__ void rope_chunk(const RopeTable& r, int position, const __nv_bfloat16* row, int c, float (&x)[8]) {
+    unpack_bf16x8(*reinterpret_cast<const uint4*>(row + 8 * c), x);
+    if (8 * c >= r.dim) return;
+    if (r.half) {
+        const int half = r.dim / 2;
+        const bool second = 8 * c >= half;
+        float y[8];
+        unpack_bf16x8(*reinterpret_cast<const uint4*>(row + (second ? 8 * c - half : 8 * c + half)), y);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float2 a = rope_angle(r, position, (second ? 8 * c - half : 8 * c) + i);
+            float p = second ? y[i] : x[i], q = second ? x[i] : y[i];
+            rope_turn(p, q, a.x, a.y);
+            x[i] = second ? q : p;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 a = rope_angle(r, position, 4 * c + i);
+            rope_turn(x[2 * i], x[2 * i + 1], a.x, a.y);
         }
     }
 }
