@@ -225,6 +225,20 @@ int bf1_decode_fwd(const void *q, const void *k_pages, const void *v_pages, int3
                    float softmax_scale, const bf1_decode_plan *plan /* host */, void *workspace,
                    void *o, float *lse, void *stream);
 
+/* The same step over a cache in 8 bits: k_pages / v_pages hold e4m3 numbers, [num_pages, 64, hkv, d], each page and KV head under
+ * an fp32 scale, [num_pages, hkv] (value = number * scale; bf1_cache_write makes powers of two, any are taken).  Half the bytes
+ * of the bf16 cache are read; scores, softmax and sums are in 32 bits, the numbers themselves enter the products exactly and P
+ * rounded to 11 bits.  Lists may be of any length (the plan's max_degree is not limited to 64), so that layers which stay dense
+ * are served too: plan them with the route {64, local_blocks >= max_pages_per_seq, 0, 0}.
+ *   workspace    device, 16-byte aligned, bf1_decode_fp8_workspace_bytes() bytes, whatever they hold.  It carries a call's partial
+ *                results: calls that may overlap on the GPU need one each
+ * All else as bf1_decode_fwd; num_pages must be positive. */
+int64_t bf1_decode_fp8_workspace_bytes(int32_t batch, int32_t hq, int32_t hkv, int32_t max_degree, int32_t d);
+int bf1_decode_fwd_fp8(const void *q, const void *k_pages, const void *v_pages, const float *k_scales, const float *v_scales,
+                       int32_t num_pages, const int32_t *seqlens_dev, int32_t batch, int32_t hq, int32_t hkv, int32_t d,
+                       float softmax_scale, const bf1_decode_plan *plan /* host */, void *workspace, void *o, float *lse,
+                       void *stream);
+
 /* ---- backward over the same route (Section 4.2's gates include a backward pass with finite
  * Q, K and V gradients) ---------------------------------------------------------------------------
  * Given the forward's inputs, its outputs o and lse, and the upstream gradient d_o [T, hq, d] bf16,

@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libbf1.so")
 HOST_SOURCE = os.path.join(CSRC, "bf1_host.cpp")
 SOURCES = ["bf1_plan.cu", "bf1_attn.cu", "bf1_noalloc.cu", "bf1_decode.cu", "bf1_bwd.cu", "bf1_shard.cu",
-           "bf1_rope.cu", "bf1_cache.cu"]
+           "bf1_rope.cu", "bf1_cache.cu", "bf1_decode8.cu"]
 HEADERS = ["bf1_common.cuh", "bf1_rope.cuh", os.path.join("..", "..", "include", "bf1.h")]
 
 

@@ -875,6 +875,22 @@ int make_map_4d(CUtensorMap* m, const void* ptr, int64_t T, int H, int d, int he
     return make_map(m, ptr, T, H, d, heads_per_box, kBlock, chunks_per_box);
 }
 
+// Pages of an 8-bit cache [pages, 64, H, d] as 3-D {d bytes, H heads, 64 * pages rows}; box = one head of one page, 64 rows of d
+// bytes, swizzled over the width of a row.
+int make_page_map(CUtensorMap* m, const void* ptr, int64_t pages, int H, int d) {
+    EncodeTiledFn enc;
+    if (int rc = get_encode_fn(&enc)) return rc;
+    cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)H, (cuuint64_t)pages * 64};
+    cuuint64_t strides[2] = {(cuuint64_t)d, (cuuint64_t)H * d};
+    cuuint32_t box[3] = {(cuuint32_t)d, 1, 64};
+    cuuint32_t estr[3] = {1, 1, 1};
+    CUresult r = enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                     d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(BF1_ERR_CUDA, "cuTensorMapEncodeTiled (pages) failed with CUresult %d", (int)r);
+    return BF1_OK;
+}
+
 struct DeviceInfo {
     int sm_count = 0;
 };

@@ -1,0 +1,544 @@
+// One-token decode over a paged cache in 8 bits: pages of e4m3 numbers, one fp32 scale for each page and KV head.
+//
+//   o = sum_i p_i sv(i) v_i / sum_i p_i,   p_i = exp(scale * sk(i) <q, k_i>),   i over the keys of the plan's pages
+//
+// Every key costs 2 d bytes and 4 d G operations: bound by HBM for as long as the arithmetic on a page (16 KB of K and V at
+// d = 128) stays hidden behind the copies, 700 cycles of an SM.  The list of a dense layer has hundreds of pages and lists are of all
+// lengths, so the work is not dealt by lists: for every KV head the pages of all lists stand in one row, which is cut into equal runs, one
+// to a CTA, as many as the SMs hold at once.  The eight CTAs that read the heads of one page run side by side, so that its 8 KB
+// rows are fetched together.  A list that a cut goes through is left as partial (max, sum, O), which a second small kernel adds up
+// in list order.
+//
+// In a CTA one warp asks for pages by TMA into a ring, and four warps take 16 keys of every page each.  The numbers of the cache are the A
+// operand of m16n8k16 (16 keys or 16 dimensions to a row, the heads are the eight columns): widened from e4m3 to f16, which is
+// exact, two at a time.  q, eight bits of fraction in bf16, is exact in f16 too once it is scaled to the head's largest value; P in f16 is rounded
+// by 2^-12, an eighth of what bf16 would cost.  Scales stay outside of the products, in 32 bits: sk on the scores, sv on each page's sum.
+#include <math.h>
+
+#include <algorithm>
+#include <atomic>
+#include <cfloat>
+#include <cuda.h>
+
+#include "bf1_common.cuh"
+
+namespace bf1 {
+
+constexpr int kP8 = 64;                  // tokens per page
+constexpr int kD8Consumers = 128, kD8Threads = kD8Consumers + 32;
+constexpr int kD8MaxStages = 8;
+constexpr int kD8MaxScan = 1024;         // sequences whose lists are cut (more of them: a CTA per list)
+constexpr int kD8MaxRuns = 640;          // runs at most, which is what the workspace has room for
+
+struct Decode8Args {
+    const __nv_bfloat16* q;              // [batch, hq, d]
+    const float *k_scales, *v_scales;    // [pages, hkv]
+    const int32_t *seqlens, *count, *page, *block;
+    int32_t* status;
+    int32_t max_degree, hq, hkv, num_pages, group, batch;
+    float scale_log2;
+    __nv_bfloat16* o;                    // [batch, hq, d]
+    float* lse;                          // [hq, batch]
+    int32_t runs;                        // per KV head; 0: a CTA per list
+    int32_t stages;
+    int32_t* bases;                      // workspace: [batch + 1] pages in front of every list
+    float2* part_ml;                     // [hkv][runs][2][group] (max, sum) ...
+    float* part_o;                       // [hkv][runs][2][group][d] ... and sum of a cut list's part
+};
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, int c0, int c1, int c2, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+        "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4_trans(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+// Two e4m3 numbers of the low / high half of a word as f16x2.
+__device__ __forceinline__ uint32_t widen_lo(uint32_t v) {
+    uint32_t r;
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\t}" : "=r"(r) : "r"(v));
+    return r;
+}
+__device__ __forceinline__ uint32_t widen_hi(uint32_t v) {
+    uint32_t r;
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, b;\n\t}" : "=r"(r) : "r"(v));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kD8Consumers) : "memory"); }
+
+// The 16-byte chunk `c` of row r of a page in shared memory, rows of D bytes, as TMA swizzles them (128 B or 64 B).
+template <int D>
+__device__ __forceinline__ uint32_t page_chunk(int r, int c) {
+    return r * D + ((c ^ (D == 128 ? r & 7 : (r >> 1) & 3)) << 4);
+}
+
+// The queries of a list's heads as the B operand of the scores: column gid is head gid, and the four values that a lane holds of
+// chunk c are the dimensions 16 c + 4 tig .. + 3, the order in which ldmatrix hands out K's bytes.  Scaled by a power of two that puts the
+// head's largest value into [2^14, 2^15): what is above 2^-38 of it has all its digits.  f[0], f[1]: what the scores of heads 2 tig and
+// 2 tig + 1 have to be multiplied with (the softmax's scale and log2 e in it).
+template <int D>
+__device__ __forceinline__ void load_queries(const Decode8Args& a, int s, int hbase, uint32_t (&qb)[D / 16][2], float (&f)[2]) {
+    const int lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
+    float x[D / 16][4], top = 0.f;
+    const uint2* row = reinterpret_cast<const uint2*>(a.q + ((size_t)s * a.hq + hbase + (gid < a.group ? gid : 0)) * D);
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) {
+        const uint2 v = gid < a.group ? row[c * 4 + tig] : make_uint2(0u, 0u);
+        x[c][0] = __uint_as_float(v.x << 16);
+        x[c][1] = __uint_as_float(v.x & 0xffff0000u);
+        x[c][2] = __uint_as_float(v.y << 16);
+        x[c][3] = __uint_as_float(v.y & 0xffff0000u);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, fabsf(x[c][i]));
+    }
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const int e = max((int)(__float_as_uint(top) >> 23) - 127, -100);              // 128 if it is infinite
+    const float up = __uint_as_float((uint32_t)(127 + 14 - e) << 23);              // 2^(14 - e)
+    const float down = a.scale_log2 * __uint_as_float((uint32_t)(127 - 14 + e) << 23);
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) {
+        qb[c][0] = pack_f16x2(x[c][0] * up, x[c][1] * up);
+        qb[c][1] = pack_f16x2(x[c][2] * up, x[c][3] * up);
+    }
+    f[0] = __shfl_sync(0xffffffffu, down, 8 * tig);                                // lanes 4 h hold head h
+    f[1] = __shfl_sync(0xffffffffu, down, 8 * tig + 4);
+}
+
+// One warp's softmax over the keys it has seen: lanes hold heads 2 tig and 2 tig + 1.
+template <int D>
+struct WarpState {
+    float m[2], l[2], acc[D / 16][4];    // acc[c]: dimensions 16 c + 2 gid (0, 1) and 16 c + 2 gid + 1 (2, 3) of the two heads
+    __device__ __forceinline__ void clear() {
+        m[0] = m[1] = -INFINITY;
+        l[0] = l[1] = 0.f;
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) acc[c][0] = acc[c][1] = acc[c][2] = acc[c][3] = 0.f;
+    }
+};
+
+// Keys key0 .. key0 + 15 of a page in shared memory, of which the first `valid` of the page count.
+template <int D>
+__device__ __forceinline__ void page_step(WarpState<D>& w, uint32_t kb, uint32_t vb, int key0, int valid, const uint32_t (&qb)[D / 16][2],
+                                          const float (&f)[2], float2 scales) {
+    const int lane = threadIdx.x & 31, gid = lane >> 2;
+    const int row = key0 + (lane & 15), odd = lane >> 4;     // ldmatrix: keys 0-7 and 8-15 of one chunk, then of the next
+    if (valid < key0 + 16) {                                 // rows behind the newest token may hold anything, NaN included
+        for (int i = lane; i < 16 * (D / 16); i += 32)
+            if (key0 + i / (D / 16) >= valid) st_shared_v4(vb + (key0 + i / (D / 16)) * D + i % (D / 16) * 16, 0u, 0u, 0u, 0u);
+        fence_proxy_async();                                 // (the next copy into this place comes behind these)
+        __syncwarp();
+    }
+    float sc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < D / 16; c += 2) {
+        uint32_t r[4];
+        ldsm4(kb + page_chunk<D>(row, c + odd), r);
+        mma_f16(sc, widen_lo(r[0]), widen_lo(r[1]), widen_hi(r[0]), widen_hi(r[1]), qb[c][0], qb[c][1]);
+        mma_f16(sc, widen_lo(r[2]), widen_lo(r[3]), widen_hi(r[2]), widen_hi(r[3]), qb[c + 1][0], qb[c + 1][1]);
+    }
+    // keys gid (0, 1) and gid + 8 (2, 3) of heads 2 tig and 2 tig + 1
+    float mx[2], al[2], base[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const float by = f[h] * scales.x;
+        sc[h] = key0 + gid < valid ? sc[h] * by : -INFINITY;
+        sc[2 + h] = key0 + gid + 8 < valid ? sc[2 + h] * by : -INFINITY;
+        mx[h] = fmaxf(sc[h], sc[2 + h]);
+    }
+#pragma unroll
+    for (int off = 4; off < 32; off <<= 1)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], off));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const float m = fmaxf(w.m[h], mx[h]);
+        base[h] = m == -INFINITY ? 0.f : m;                  // (scores of minus infinity alone)
+        al[h] = ex2_approx(w.m[h] - base[h]);
+        w.m[h] = m;
+        sc[h] = ex2_approx(sc[h] - base[h]);
+        sc[2 + h] = ex2_approx(sc[2 + h] - base[h]);
+        w.l[h] = fmaf(w.l[h], al[h], sc[h] + sc[2 + h]);
+    }
+    const bool rescale = __any_sync(0xffffffffu, al[0] != 1.f || al[1] != 1.f);
+    const uint32_t b0 = transpose8x8(pack_f16x2(sc[0], sc[1])), b1 = transpose8x8(pack_f16x2(sc[2], sc[3]));
+#pragma unroll
+    for (int c = 0; c < D / 16; c += 2) {
+        uint32_t r[4];
+        ldsm4_trans(vb + page_chunk<D>(row, c + odd), r);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = __byte_perm(r[i], 0, 0x3120);     // (two keys of one dimension side by side)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            float pa[4] = {0.f, 0.f, 0.f, 0.f};
+            mma_f16(pa, widen_lo(r[2 * u]), widen_hi(r[2 * u]), widen_lo(r[2 * u + 1]), widen_hi(r[2 * u + 1]), b0, b1);
+            float(&acc)[4] = w.acc[c + u];
+            if (rescale) acc[0] *= al[0], acc[1] *= al[1], acc[2] *= al[0], acc[3] *= al[1];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[i] = fmaf(scales.y, pa[i], acc[i]);
+        }
+    }
+}
+
+template <int D, int kHeads>
+struct Merge8 {                          // the four warps' states at the end of a list or a part of it
+    float o[4][kHeads][D + 4], m[4][kHeads], l[4][kHeads];
+};
+
+// grid (hkv, runs), or (hkv, batch) with runs = 0
+template <int D, int kHeads>
+__global__ void __launch_bounds__(kD8Threads, 3) decode8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                                                                const Decode8Args a) {
+    constexpr int kPageBytes = kP8 * D;
+    extern __shared__ uint8_t dsmem[];
+    __shared__ uint64_t bars[2 * kD8MaxStages];
+    __shared__ float2 page_scales[kD8MaxStages];
+    __shared__ Merge8<D, kHeads> st;
+    __shared__ int warp_sums[kD8Threads / 32];
+    __shared__ int abort_flag;
+    const uint32_t ring = (smem_u32(dsmem) + 1023) & ~1023u;
+    int* const bases = reinterpret_cast<int*>(dsmem + (ring - smem_u32(dsmem)) + (size_t)a.stages * 2 * kPageBytes);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, kvh = blockIdx.x;
+    const uint32_t full = smem_u32(bars), empty = full + 8 * kD8MaxStages;
+    if (tid == 0) {
+        abort_flag = 0;
+        for (int i = 0; i < a.stages; ++i) {
+            mbar_init(full + 8 * i, 1);
+            mbar_init(empty + 8 * i, kD8Consumers / 32);
+        }
+        fence_mbar_init();
+        tma_prefetch_desc(&tm_k);
+        tma_prefetch_desc(&tm_v);
+    }
+    pdl_wait();
+    // ---- the pages in front of every list ------------------------------------------------------------------------------------------
+    auto pages_of_list = [&](int s) {
+        const int n = a.seqlens[s];
+        const int c = max(min(a.count[s], a.max_degree), 0);
+        if (c > 0 && (n < 1 || (n - 1) / kP8 != a.block[s])) {       // the plan belongs to another 64 tokens
+            if (kvh == 0 && (a.runs == 0 || blockIdx.y == 0)) atomicOr(a.status, BF1_DEV_BAD_ROUTE);
+            return 0;
+        }
+        return c;
+    };
+    int s = 0, x0 = 0, x1 = 0;
+    if (a.runs == 0) {
+        s = blockIdx.y;
+        if (tid == 0) {
+            const int c = pages_of_list(s);
+            bases[0] = 0;
+            bases[1] = c;
+        }
+        __syncthreads();
+        x1 = bases[1];
+    } else {
+        const int per = (a.batch + kD8Threads - 1) / kD8Threads, lo = min(tid * per, a.batch), hi = min(lo + per, a.batch);
+        int sum = 0;
+        for (int i = lo; i < hi; ++i) {
+            const int c = pages_of_list(i);
+            bases[i] = c;
+            sum += c;
+        }
+        int incl = sum;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, incl, off);
+            if (lane >= off) incl += v;
+        }
+        if (lane == 31) warp_sums[warp] = incl;
+        __syncthreads();
+        int at = incl - sum;
+        for (int w = 0; w < warp; ++w) at += warp_sums[w];
+        for (int i = lo; i < hi; ++i) {
+            const int c = bases[i];
+            bases[i] = at;
+            at += c;
+        }
+        if (lo < hi && hi == a.batch) bases[a.batch] = at;
+        __syncthreads();
+        const long long total = bases[a.batch];
+        const int runs = (int)min((long long)a.runs, total);         // none of them empty
+        if ((int)blockIdx.y < runs) {
+            x0 = (int)(total * blockIdx.y / runs);
+            x1 = (int)(total * (blockIdx.y + 1) / runs);
+        }
+        if (kvh == 0 && blockIdx.y == 0)
+            for (int i = tid; i <= a.batch; i += kD8Threads) a.bases[i] = bases[i];
+    }
+    if (x0 >= x1) return;
+    // the list that page x belongs to
+    auto list_of = [&](int x) {
+        int lo = 0, hi = a.batch;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (bases[mid] <= x) lo = mid;
+            else hi = mid;
+        }
+        return lo;
+    };
+    if (warp == kD8Consumers / 32) {
+        // ---- the copying warp: a lane looks up a page and its scales, 32 pages ahead of their use -------------------------------------
+        auto look_up = [&](int x, int& pg, float2& sc) {
+            pg = 0;
+            sc = make_float2(0.f, 0.f);
+            if (x >= x1) return;
+            const int sx = a.runs == 0 ? s : list_of(x);
+            pg = a.page[(size_t)sx * a.max_degree + (x - (a.runs == 0 ? 0 : bases[sx]))];
+            if (pg < 0 || pg >= a.num_pages) {
+                atomicOr(a.status, BF1_DEV_BAD_ROUTE);
+                pg = 0;
+            }
+            sc = make_float2(a.k_scales[(size_t)pg * a.hkv + kvh], a.v_scales[(size_t)pg * a.hkv + kvh]);
+        };
+        int pg, stage = 0, parity = 1, issued = 0;
+        bool ok = true;
+        float2 sc;
+        look_up(x0 + lane, pg, sc);
+        for (int xb = x0; xb < x1 && ok; xb += 32) {
+            int pg_next;
+            float2 sc_next;
+            look_up(xb + 32 + lane, pg_next, sc_next);
+            const int n = min(32, x1 - xb);
+            for (int i = 0; i < n; ++i) {
+                const int p = __shfl_sync(0xffffffffu, pg, i);
+                const float2 ps = make_float2(__shfl_sync(0xffffffffu, sc.x, i), __shfl_sync(0xffffffffu, sc.y, i));
+                // (a barrier that has not completed a phase lets a wait for parity 1 pass: the ring is empty at first)
+                ok = __all_sync(0xffffffffu, mbar_wait(empty + 8 * stage, parity, &abort_flag, a.status));
+                if (!ok) break;
+                if (lane == 0) {
+                    const uint32_t bar = full + 8 * stage, to = ring + stage * 2 * kPageBytes;
+                    page_scales[stage] = ps;
+                    mbar_expect_tx(bar, 2 * kPageBytes);
+                    tma_load_3d(to, &tm_k, 0, kvh, p * kP8, bar);
+                    tma_load_3d(to + kPageBytes, &tm_v, 0, kvh, p * kP8, bar);
+                }
+                __syncwarp();
+                ++issued;
+                if (++stage == a.stages) stage = 0, parity ^= 1;
+            }
+            pg = pg_next;
+            sc = sc_next;
+        }
+        if (!ok) {                                           // given up: the copies on their way have to land all the same
+            const long long t0 = clock64();
+            for (int i = max(0, issued - a.stages); i < issued; ++i)
+                while (!mbar_try_wait(full + 8 * (i % a.stages), i / a.stages & 1) && clock64() - t0 < kWaitCycles) {
+                }
+        }
+        return;
+    }
+    // ---- the four warps that compute: one list, or the part of it that lies in this run, after the other ----------------------------------
+    const int key0 = warp * 16, hbase = kvh * a.group, gid = lane >> 2, tig = lane & 3;
+    int stage = 0, parity = 0;
+    if (a.runs != 0) s = list_of(x0);
+    for (int x = x0; x < x1;) {
+        if (a.runs != 0)
+            while (bases[s + 1] <= x) ++s;                   // (empty lists)
+        const int first = a.runs == 0 ? 0 : bases[s], last = a.runs == 0 ? x1 : bases[s + 1], end = min(x1, last);
+        const bool head = x == first, whole = head && end == last;
+        const int n = a.seqlens[s], tail = n - (n - 1) / kP8 * kP8;
+        uint32_t qb[D / 16][2];
+        float f[2];
+        load_queries<D>(a, s, hbase, qb, f);
+        WarpState<D> w;
+        w.clear();
+        for (; x < end; ++x) {
+            mbar_wait(full + 8 * stage, parity, &abort_flag, a.status);
+            const int valid = x == last - 1 ? tail : kP8;
+            const uint32_t kb = ring + stage * 2 * kPageBytes;
+            if (key0 < valid) page_step<D>(w, kb, kb + kPageBytes, key0, valid, qb, f, page_scales[stage]);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(empty + 8 * stage);
+            if (++stage == a.stages) stage = 0, parity ^= 1;
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int off = 4; off < 32; off <<= 1) w.l[h] += __shfl_xor_sync(0xffffffffu, w.l[h], off);
+        if (2 * tig < kHeads) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (gid == 0) {
+                    st.m[warp][2 * tig + h] = w.m[h];
+                    st.l[warp][2 * tig + h] = w.l[h];
+                }
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c)
+                    *reinterpret_cast<float2*>(&st.o[warp][2 * tig + h][16 * c + 2 * gid]) = make_float2(w.acc[c][h], w.acc[c][2 + h]);
+            }
+        }
+        consumers_sync();
+        constexpr int kCols = kHeads * D / kD8Consumers, kPerHead = kD8Consumers / kHeads;
+        const int h = tid / kPerHead, c0 = tid % kPerHead * kCols;
+        if (h < a.group) {
+            const float m = fmaxf(fmaxf(st.m[0][h], st.m[1][h]), fmaxf(st.m[2][h], st.m[3][h]));
+            const float base = m == -INFINITY ? 0.f : m;
+            float l = 0.f, out[kCols] = {};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float by = exp2f(st.m[i][h] - base);   // 0 for a warp that has seen no key
+                l = fmaf(by, st.l[i][h], l);
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) out[c] = fmaf(by, st.o[i][h][c0 + c], out[c]);
+            }
+            if (whole) {
+                const float inv = 1.f / l;
+                __nv_bfloat16* orow = a.o + ((size_t)s * a.hq + hbase + h) * D + c0;
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) orow[c] = __float2bfloat16_rn(out[c] * inv);
+                if (c0 == 0) a.lse[(size_t)(hbase + h) * a.batch + s] = (m + log2f(l)) * 0.6931471805599453f;
+            } else {
+                // a run cuts at most two lists: the one it begins in and the one it ends in
+                const size_t slot = (((size_t)kvh * a.runs + blockIdx.y) * 2 + (head ? 1 : 0)) * a.group + h;
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) a.part_o[slot * D + c0 + c] = out[c];
+                if (c0 == 0) a.part_ml[slot] = make_float2(m, l);
+            }
+        }
+        consumers_sync();                                    // (the states are written again)
+    }
+}
+
+// Adds up the lists that cuts go through: a CTA per list and KV head.  Parts stand in list order, run by run.
+constexpr int kJoinThreads = 256;
+template <int D>
+__global__ void __launch_bounds__(kJoinThreads) decode8_join_kernel(const Decode8Args a) {
+    constexpr int kVec = D / 4;                              // threads to a head's row, 4 columns each
+    __shared__ float4 sums[kJoinThreads];
+    pdl_wait();
+    const int kvh = blockIdx.x, s = blockIdx.y, tid = threadIdx.x;
+    const long long total = a.bases[a.batch], first = a.bases[s], last = a.bases[s + 1];
+    if (first == last) return;
+    const long long runs = min((long long)a.runs, total);
+    auto run_of = [&](long long x) { return (int)(((x + 1) * runs - 1) / total); };   // the last run that begins at or in front of page x
+    const int j0 = run_of(first), j1 = run_of(last - 1);
+    if (j0 == j1) return;                                    // whole: written already
+    const int columns = a.group * kVec, groups = kJoinThreads / columns;
+    const int g = tid / columns, h = tid % columns / kVec, c = tid % kVec;
+    auto slot = [&](int j) { return (((size_t)kvh * a.runs + j) * 2 + (j == j0 ? 1 : 0)) * a.group + h; };
+    float m = -INFINITY;
+    for (int j = j0; j <= j1; ++j) m = fmaxf(m, a.part_ml[slot(j)].x);
+    const float base = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int j = j0; j <= j1; ++j) {
+        const float2 ml = a.part_ml[slot(j)];
+        const float by = exp2f(ml.x - base);
+        l = fmaf(by, ml.y, l);
+        if ((j - j0) % groups == g) {
+            const float4 v = *reinterpret_cast<const float4*>(a.part_o + slot(j) * D + 4 * c);
+            o.x = fmaf(by, v.x, o.x), o.y = fmaf(by, v.y, o.y), o.z = fmaf(by, v.z, o.z), o.w = fmaf(by, v.w, o.w);
+        }
+    }
+    sums[tid] = o;
+    __syncthreads();
+    if (g > 0) return;
+    for (int i = 1; i < groups; ++i) {
+        const float4 v = sums[i * columns + tid];
+        o.x += v.x, o.y += v.y, o.z += v.z, o.w += v.w;
+    }
+    const float inv = 1.f / l;
+    *reinterpret_cast<uint2*>(a.o + ((size_t)s * a.hq + kvh * a.group + h) * D + 4 * c) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+    if (c == 0) a.lse[(size_t)(kvh * a.group + h) * a.batch + s] = (m + log2f(l)) * 0.6931471805599453f;
+}
+
+int make_page_map(CUtensorMap* m, const void* ptr, int64_t pages, int hkv, int d);   // bf1_attn.cu
+
+typedef void (*Decode8Kernel)(CUtensorMap, CUtensorMap, Decode8Args);
+static size_t up16(size_t x) { return (x + 15) / 16 * 16; }
+
+}  // namespace bf1
+
+using namespace bf1;
+
+// [bases | (max, sum) | O] of at most two parts to a run
+extern "C" int64_t bf1_decode_fp8_workspace_bytes(int32_t batch, int32_t hq, int32_t hkv, int32_t max_degree, int32_t d) {
+    if (batch < 0 || hq <= 0 || hkv <= 0 || hq % hkv != 0 || max_degree <= 0 || d <= 0) return -1;
+    if (batch > kD8MaxScan) return 16;
+    const size_t parts = (size_t)std::max(1, kD8MaxRuns / hkv) * hkv * 2 * (hq / hkv);
+    return (int64_t)(up16(sizeof(int32_t) * ((size_t)batch + 1)) + parts * (sizeof(float2) + sizeof(float) * d));
+}
+
+extern "C" int bf1_decode_fwd_fp8(const void* q, const void* k_pages, const void* v_pages, const float* k_scales, const float* v_scales,
+                                  int32_t num_pages, const int32_t* seqlens_dev, int32_t batch, int32_t hq, int32_t hkv, int32_t d,
+                                  float softmax_scale, const bf1_decode_plan* plan, void* workspace, void* o, float* lse, void* stream) {
+    if (!q || !k_pages || !v_pages || !k_scales || !v_scales || !seqlens_dev || !plan || !workspace || !o || !lse)
+        return fail(BF1_ERR_INVALID_ARG, "a pointer is null");
+    if (!plan->count || !plan->page || !plan->block || !plan->status) return fail(BF1_ERR_INVALID_ARG, "a decode-plan pointer is null");
+    if (batch < 0 || num_pages < 1 || hq <= 0 || hkv <= 0) return fail(BF1_ERR_INVALID_ARG, "negative or zero size argument");
+    if (hq % hkv != 0) return fail(BF1_ERR_INVALID_ARG, "hq %d is not a multiple of hkv %d", hq, hkv);
+    const int group = hq / hkv;
+    if (group != 1 && group != 2 && group != 4) return fail(BF1_ERR_UNSUPPORTED, "GQA group size %d: only G = 1, 2 and 4 are supported", group);
+    if (d != 64 && d != 128) return fail(BF1_ERR_UNSUPPORTED, "head dimension %d: only 64 and 128 are supported", d);
+    if (((uintptr_t)q | (uintptr_t)k_pages | (uintptr_t)v_pages | (uintptr_t)o | (uintptr_t)workspace) & 15)
+        return fail(BF1_ERR_INVALID_ARG, "q, k_pages, v_pages, o and workspace must be 16-byte aligned");
+    if (plan->max_degree < 1 || batch > 65535 || hkv > 65535 || num_pages > (1 << 25) - 1 || (int64_t)plan->max_degree * std::min(batch, kD8MaxScan) > 0x7fffffffLL)
+        return fail(BF1_ERR_UNSUPPORTED, "batch and KV heads up to 65535, pages up to 2^25 - 1, pages of all lists below 2^31");
+    if (batch == 0) return BF1_OK;
+    Decode8Args a;
+    a.q = (const __nv_bfloat16*)q;
+    a.k_scales = k_scales;
+    a.v_scales = v_scales;
+    a.seqlens = seqlens_dev;
+    a.count = plan->count;
+    a.page = plan->page;
+    a.block = plan->block;
+    a.status = plan->status;
+    a.max_degree = plan->max_degree;
+    a.hq = hq;
+    a.hkv = hkv;
+    a.num_pages = num_pages;
+    a.group = group;
+    a.batch = batch;
+    a.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)d)) * 1.4426950408889634f;
+    a.o = (__nv_bfloat16*)o;
+    a.lse = lse;
+    int dev = 0;
+    BF1_CUDA_CHECK(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= 64) return fail(BF1_ERR_NO_DEVICE, "device ordinal %d out of range", dev);
+    static const Decode8Kernel kernels[4] = {decode8_kernel<64, 2>, decode8_kernel<128, 2>, decode8_kernel<64, 4>, decode8_kernel<128, 4>};
+    const int which = (group == 4 ? 2 : 0) + (d == 128);
+    constexpr int kMostSmem = 100 * 1024;
+    static std::atomic<int> sm_count[64];      // 0: this device has not been set up
+    int sms = sm_count[dev].load(std::memory_order_acquire);
+    if (!sms) {
+        for (Decode8Kernel k : kernels) BF1_CUDA_CHECK(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem));
+        BF1_CUDA_CHECK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+        sm_count[dev].store(sms, std::memory_order_release);
+    }
+    a.runs = batch > kD8MaxScan ? 0 : std::max(1, std::min(3 * sms, kD8MaxRuns) / hkv);
+    a.stages = d == 128 ? 3 : 6;
+    a.bases = (int32_t*)workspace;
+    a.part_ml = (float2*)((uint8_t*)workspace + up16(sizeof(int32_t) * ((size_t)batch + 1)));
+    a.part_o = (float*)(a.part_ml + (size_t)hkv * a.runs * 2 * group);
+    CUtensorMap tk, tv;
+    if (int rc = make_page_map(&tk, k_pages, num_pages, hkv, d)) return rc;
+    if (int rc = make_page_map(&tv, v_pages, num_pages, hkv, d)) return rc;
+    const size_t smem = 1024 + (size_t)a.stages * 2 * kP8 * d + sizeof(int) * ((a.runs ? batch : 1) + 1);
+    BF1_CUDA_CHECK(launch_pdl(kernels[which], dim3(hkv, a.runs ? a.runs : batch), kD8Threads, smem, (cudaStream_t)stream, tk, tv, a));
+    if (a.runs)
+        BF1_CUDA_CHECK(launch_pdl(d == 128 ? decode8_join_kernel<128> : decode8_join_kernel<64>, dim3(hkv, batch), kJoinThreads, 0,
+                                  (cudaStream_t)stream, a));
+    return BF1_OK;
+}

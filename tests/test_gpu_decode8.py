@@ -1,0 +1,368 @@
+"""One-token decode over 8-bit pages against 64 bits: tails, empty sequences, long and short lists, cut ones, what lies behind the
+newest token, scales and queries of all sizes, and a serving loop that fills the cache it reads."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_20427_b200 as bf1
+from oracle import cache_oracle as C
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda:0")
+E4M3 = torch.float8_e4m3fn
+DENSE = dict(block=64, local_blocks=1 << 20, global_first=0, dyadic=0)
+
+
+def logical(n, dense):
+    j = (n - 1) // 64
+    if n == 0:
+        return []
+    if dense:
+        return list(range(j + 1))
+    return sorted({j, 0} | {j - w for w in (1, 2) if w <= j} | {j - (1 << k) for k in range(20) if j >= 1 << k})
+
+
+class Cache:
+    """Pages of random numbers; `lens` tokens per sequence, pages in random order."""
+
+    def __init__(self, lens, hkv, d, dense, seed, room=5, exponents=(-9, -5)):
+        g = torch.Generator().manual_seed(seed)
+        self.lens = lens
+        self.lists = [logical(n, dense) for n in lens]
+        held = [(n + 63) // 64 for n in lens]
+        need = sum(len(x) for x in self.lists)
+        perm = [int(x) for x in torch.randperm(need + room, generator=g)]
+        table = torch.full((len(lens), max(max(held), 1)), -1, dtype=torch.int32)
+        for s, x in enumerate(self.lists):
+            for b in x:
+                table[s, b] = perm.pop()
+        self.lists = [[int(table[s, b]) for b in x] for s, x in enumerate(self.lists)]
+        shape = (need + room, 64, hkv, d)
+        self.kp, self.vp = ((torch.randn(shape, generator=g) * 60).clamp(-448, 448).to(E4M3) for _ in range(2))
+        self.ks, self.vs = (2.0 ** torch.randint(*exponents, shape[:1] + (hkv,), generator=g).float() for _ in range(2))
+        self.table = table
+        self.cfg = bf1.RouteCfg(**DENSE) if dense else bf1.RouteCfg()
+
+    def garbage_behind(self):
+        """NaN wherever nothing has been written."""
+        used = {p for x in self.lists for p in x}
+        for t in (self.kp, self.vp):
+            u = t.view(torch.uint8)
+            for p in range(u.shape[0]):
+                if p not in used:
+                    u[p] = 0x7f
+            for x, n in zip(self.lists, self.lens):
+                if n % 64:
+                    u[x[-1], n % 64:] = 0xff
+        for t in (self.ks, self.vs):
+            for p in range(t.shape[0]):
+                if p not in used:
+                    t[p] = float("nan")
+
+
+def run(c, q, scale=None, plan=None, times=2):
+    lens = torch.tensor(c.lens, dtype=torch.int32, device=DEV)
+    plan = plan or bf1.plan_decode(lens, c.table.to(DEV), c.cfg)
+    batch, hq, d = q.shape
+    ws = bf1.decode_fp8_workspace(batch, hq, c.kp.shape[2], plan.max_degree, d, DEV)
+    ws.fill_(0xff)                                                 # NaN, whatever it is read as
+    out = torch.full((batch, hq, d), float("nan"), dtype=torch.bfloat16, device=DEV)
+    lse = torch.full((hq, batch), float("nan"), device=DEV)
+    args = [t.to(DEV) for t in (q, c.kp, c.vp, c.ks, c.vs)]
+    first = None
+    for _ in range(times):
+        bf1.decode_fwd_fp8(*args, lens, plan, ws, scale=scale, out=out, lse=lse)
+        torch.cuda.synchronize()
+        first = first or (out.clone(), lse.clone())
+    assert torch.equal(first[0].view(torch.int16), out.view(torch.int16)) and torch.equal(first[1].view(torch.int32), lse.view(torch.int32))
+    return out, lse, plan
+
+
+def check(c, q, out, lse, scale=None):
+    """What may be off: the result's rounding, 2^-8 of it; the weights' rounding to f16, 2^-11 of each (below 2^-14 of the largest 2^-25 in all);
+    a score, by the sum of its d products in 32 bits (d 2^-24 of their absolute sum), and by its product with two scales and its difference to the
+    maximum (2^-21 of the largest score); an exponential, 2^-22.  The weights' errors count on the mean of |v|."""
+    q64, kp, vp, ks, vs = (t.double().cpu().numpy() for t in (q, c.kp, c.vp, c.ks, c.vs))
+    batch, hq, d = q.shape
+    group = hq // kp.shape[2]
+    want, want_lse = C.decode(q64, kp, vp, ks, vs, c.lists, c.lens, scale)
+    by = scale or 1 / math.sqrt(d)
+    got, got_lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    for s, (x, n) in enumerate(zip(c.lists, c.lens)):
+        if n == 0:
+            assert np.isnan(got[s]).all() and np.isnan(got_lse[:, s]).all()        # not written
+            continue
+        keys = (len(x) - 1) * 64 + (n - 1) % 64 + 1
+        for h in range(hq):
+            j = h // group
+            k = np.abs(kp[x, :, j] * ks[x, j][:, None, None]).reshape(-1, d)[:keys]
+            v = np.abs(vp[x, :, j] * vs[x, j][:, None, None]).reshape(-1, d)[:keys]
+            score = by * ((kp[x, :, j] * ks[x, j][:, None, None]).reshape(-1, d)[:keys] @ q64[s, h])
+            sums = by * (k @ np.abs(q64[s, h])).max()
+            off = d * 2.0 ** -24 * sums + 2.0 ** -21 * (np.abs(score).max() + 1)
+            w = np.exp(score - want_lse[h, s])
+            mean, rest = w @ v, 2.0 ** -25 * v.sum(0) * w.max()
+            limit = 2.0 ** -8 * np.abs(want[s, h]) + (2.0 ** -11 + 2 * off) * 1.01 * mean + rest
+            assert (np.abs(got[s, h] - want[s, h]) <= limit).all(), (s, h, np.abs(got[s, h] - want[s, h]).max(), limit.min())
+            assert abs(got_lse[h, s] - want_lse[h, s]) <= off + 2.0 ** -21 * (1 + abs(want_lse[h, s])), (s, h)
+
+
+def queries(batch, hq, d, seed, size=1.0):
+    return (torch.randn((batch, hq, d), generator=torch.Generator().manual_seed(seed)) * size).to(torch.bfloat16)
+
+
+@pytest.mark.parametrize("dense", [False, True], ids=["route", "dense"])
+@pytest.mark.parametrize("hq,hkv,d", [(2, 2, 64), (4, 2, 128), (8, 2, 64), (16, 8, 128), (8, 2, 128), (1, 1, 128), (6, 3, 64)])
+def test_tails_and_empty_sequences(hq, hkv, d, dense):
+    lens = [1, 64, 65, 0, 257, 1000, 0, 4097, 63, 128]
+    c = Cache(lens, hkv, d, dense, seed=hq + d)
+    q = queries(len(lens), hq, d, 1)
+    out, lse, plan = run(c, q)
+    assert plan.status.item() == 0
+    check(c, q, out, lse)
+    c.garbage_behind()
+    again, lse2, _ = run(c, q)
+    assert torch.equal(out.view(torch.int16), again.view(torch.int16)) and torch.equal(lse.view(torch.int32), lse2.view(torch.int32))
+
+
+@pytest.mark.parametrize("lens,hq,hkv,d,dense", [([1], 2, 1, 64, False), ([130], 1, 1, 64, True), ([32768], 16, 8, 128, False), ([20011], 8, 2, 64, True),
+                                                 ([40000, 3], 4, 1, 128, True), ([9000] * 3 + [1, 0, 70], 16, 4, 128, True), ([0, 0], 2, 1, 64, False),
+                                                 ([64 * 40, 0, 0, 64 * 40 + 1], 2, 2, 128, True)])
+def test_long_and_short_lists(lens, hq, hkv, d, dense):
+    """Lists that many cuts go through, runs without a page, single pages."""
+    c = Cache(lens, hkv, d, dense, seed=len(lens))
+    q = queries(len(lens), hq, d, 2)
+    out, lse, _ = run(c, q)
+    check(c, q, out, lse)
+
+
+@pytest.mark.parametrize("batch,hq,hkv", [(300, 2, 1), (1024, 2, 1), (1025, 4, 1), (1500, 2, 2)])
+def test_batches(batch, hq, hkv):
+    """Up to 1024 lists are cut into equal runs, more are walked whole."""
+    rng = np.random.default_rng(batch)
+    lens = [int(x) for x in rng.integers(0, 500, batch)]
+    c = Cache(lens, hkv, 64, False, seed=3)
+    q = queries(batch, hq, 64, 3)
+    out, lse, _ = run(c, q)
+    check(c, q, out, lse)
+
+
+def test_scales_of_all_sizes_and_a_given_softmax_scale():
+    """A page's weights are rounded against the softmax's maximum alone: a page of tiny values beside huge ones loses nothing of its own."""
+    c = Cache([1000, 64, 130], 2, 64, True, seed=4, exponents=(-9, -8))
+    c.vs *= 2.0 ** torch.randint(-60, 60, c.vs.shape, generator=torch.Generator().manual_seed(5)).float()
+    c.ks *= 1.37                                                    # no power of two
+    q = queries(3, 4, 64, 4)
+    out, lse, _ = run(c, q, scale=0.03)
+    check(c, q, out, lse, scale=0.03)
+
+
+@pytest.mark.parametrize("size", [1e-30, 1e-3, 300.0, 1e30])
+def test_queries_of_all_sizes(size):
+    c = Cache([300, 65], 1, 128, True, seed=6)
+    q = queries(2, 2, 128, 6, size)
+    c.ks = (c.ks.double() / size).float()
+    out, lse, _ = run(c, q)
+    check(c, q, out, lse)
+    assert torch.isfinite(out).all()
+
+
+def test_what_is_not_finite_stays_in_its_list():
+    """NaN in a key or a value, an infinity in a query: NaN in that sequence's and head's result, others as they were."""
+    c = Cache([200, 70, 300], 2, 64, True, seed=7)
+    q = queries(3, 4, 64, 7)
+    base, base_lse, _ = run(c, q)
+    c.kp.view(torch.uint8)[c.lists[0][1], 5, 0, 9] = 0x7f            # a key of sequence 0, KV head 0
+    c.vp.view(torch.uint8)[c.lists[2][0], 63, 1, 3] = 0xff           # a value of sequence 2, KV head 1
+    q[1, 3, 0] = float("inf")
+    out, lse, _ = run(c, q)
+    bad = torch.zeros((3, 4, 64), dtype=torch.bool)
+    bad[0, :2] = True
+    bad[2, 2:, 3] = True
+    bad[1, 3] = True
+    assert torch.isnan(out[bad.to(DEV)]).all() and torch.equal(out[~bad.to(DEV)], base[~bad.to(DEV)])
+    gone = torch.zeros((4, 3), dtype=torch.bool)
+    gone[:2, 0] = gone[3, 1] = True
+    assert torch.isnan(lse[gone.to(DEV)]).all() and torch.equal(lse[~gone.to(DEV)], base_lse[~gone.to(DEV)])
+
+
+def test_equal_scores_give_the_mean():
+    """Queries of zero: every key counts alike; the LSE is the log of their number."""
+    c = Cache([1000, 1, 64], 1, 64, True, seed=8)
+    out, lse, _ = run(c, torch.zeros((3, 2, 64), dtype=torch.bfloat16))
+    check(c, torch.zeros((3, 2, 64)), out, lse)
+    assert np.allclose(lse[0].cpu(), np.log([1000, 1, 64]), atol=1e-5)
+
+
+def test_another_64_tokens_and_bad_pages_are_reported():
+    c = Cache([100, 200], 1, 64, False, seed=9)
+    q = queries(2, 2, 64, 9)
+    lens = torch.tensor([100, 200], dtype=torch.int32, device=DEV)
+    plan = bf1.plan_decode(lens, c.table.to(DEV), c.cfg)
+    c.lens = [128, 200]                                             # still the plan's blocks
+    out, lse, _ = run(c, q, plan=plan)
+    assert plan.status.item() == 0
+    check(c, q, out, lse)
+    c.lens = [129, 200]
+    out, lse, _ = run(c, q, plan=plan)
+    assert plan.status.item() == 8 and torch.isnan(out[0]).all() and torch.isfinite(out[1]).all()
+    plan = bf1.plan_decode(lens, c.table.to(DEV), c.cfg)
+    plan.page[0, 0] = c.kp.shape[0]
+    plan.page[0, 1] = -1
+    c.lens = [100, 200]
+    out, lse, _ = run(c, q, plan=plan)                              # page 0 is read in their place
+    assert plan.status.item() == 8 and torch.isfinite(out[1]).all()
+
+
+def test_pages_beyond_32_bits():
+    hkv, d = 8, 128
+    pages = (1 << 31) // (64 * hkv * d) + 30
+    c = Cache([500, 64], hkv, d, True, seed=10)
+    n = c.kp.shape[0]
+    big = [torch.zeros((pages, 64, hkv, d), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    ks, vs = (torch.ones((pages, hkv), device=DEV) for _ in range(2))
+    for b, t in zip(big, (c.kp, c.vp)):
+        b[-n:] = t.view(torch.uint8).to(DEV)
+    ks[-n:], vs[-n:] = c.ks.to(DEV), c.vs.to(DEV)
+    q = queries(2, 16, d, 10)
+    out, lse, _ = run(c, q)
+    table = torch.where(c.table >= 0, c.table + pages - n, c.table).to(DEV)
+    lens = torch.tensor(c.lens, dtype=torch.int32, device=DEV)
+    plan = bf1.plan_decode(lens, table, c.cfg)
+    ws = bf1.decode_fp8_workspace(2, 16, hkv, plan.max_degree, d, DEV)
+    far, far_lse = bf1.decode_fwd_fp8(q.to(DEV), big[0].view(E4M3), big[1].view(E4M3), ks, vs, lens, plan, ws)
+    assert torch.equal(far, out) and torch.equal(far_lse, lse)
+
+
+def test_graph_and_another_stream():
+    c = Cache([3000, 64, 777], 2, 128, True, seed=11)
+    q = queries(3, 4, 128, 11)
+    want, want_lse, plan = run(c, q)
+    lens = torch.tensor(c.lens, dtype=torch.int32, device=DEV)
+    args = [t.to(DEV) for t in (q, c.kp, c.vp, c.ks, c.vs)] + [lens, plan]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = bf1.decode_fwd_fp8(*args, bf1.decode_fp8_workspace(3, 4, 2, plan.max_degree, 128, DEV), stream=side)
+    side.synchronize()
+    assert torch.equal(got[0], want) and torch.equal(got[1], want_lse)
+    ws = bf1.decode_fp8_workspace(3, 4, 2, plan.max_degree, 128, DEV)
+    out, lse = torch.zeros_like(want), torch.zeros_like(want_lse)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        bf1.decode_fwd_fp8(*args, ws, out=out, lse=lse)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+def test_refusals_of_the_binding():
+    c = Cache([100], 1, 64, False, seed=12)
+    q, kp, vp, ks, vs = (t.to(DEV) for t in (queries(1, 2, 64, 12), c.kp, c.vp, c.ks, c.vs))
+    lens = torch.tensor([100], dtype=torch.int32, device=DEV)
+    plan = bf1.plan_decode(lens, c.table.to(DEV), c.cfg)
+    ws = bf1.decode_fp8_workspace(1, 2, 1, plan.max_degree, 64, DEV)
+    f = bf1.decode_fwd_fp8
+    for bad in (lambda: f(q.float(), kp, vp, ks, vs, lens, plan, ws), lambda: f(q, kp.view(torch.uint8), vp, ks, vs, lens, plan, ws),
+                lambda: f(q, kp, vp[:1], ks, vs, lens, plan, ws), lambda: f(q, kp, vp, ks[:1], vs, lens, plan, ws),
+                lambda: f(q, kp, vp, ks, vs.double(), lens, plan, ws), lambda: f(q, kp, vp, ks, vs, lens.long(), plan, ws),
+                lambda: f(q, kp, vp, ks, vs, lens, plan, ws[:100]), lambda: f(q, kp.cpu(), vp, ks, vs, lens, plan, ws),
+                lambda: f(q, kp, vp, ks, vs, torch.cat((lens, lens)), plan, ws), lambda: f(q, kp, vp, ks, vs, lens, bf1.DecodePlan.empty(1, 4, "cpu"), ws),
+                lambda: f(q, kp, vp, ks, vs, lens, bf1.DecodePlan.empty(2, 4, DEV), ws), lambda: f(q, kp, vp, ks, vs, lens, plan, ws.cpu()),
+                lambda: f(q, kp, vp, ks, vs, lens, plan, ws, out=torch.zeros_like(q).float()), lambda: f(q, kp, vp, ks, vs, lens, plan, ws, lse=torch.zeros((1, 2), device=DEV))):
+        with pytest.raises(AssertionError):
+            bad()
+    with pytest.raises(bf1.Bf1Error):
+        f(torch.cat([q] * 4, 1), kp, vp, ks, vs, lens, plan, bf1.decode_fp8_workspace(1, 8, 1, plan.max_degree, 64, DEV))
+    o, lse = f(q[:0], kp, vp, ks, vs, lens[:0], bf1.DecodePlan.empty(0, 4, DEV), ws)
+    assert o.shape == (0, 2, 64) and lse.shape == (2, 0)
+
+
+@pytest.mark.parametrize("dense", [False, True], ids=["route", "dense"])
+def test_a_serving_loop(dense):
+    """Prompts, then tokens: plan_cache, rope and write, plan_decode, decode, lengths on the device all the while, one captured step;
+    every step against attention in 64 bits over the keys and values as they went in (which the cache holds to 2^-4 of each)."""
+    hq, hkv, d, pages, batch = 4, 2, 64, 40, 3
+    g = torch.Generator().manual_seed(13)
+    cfg = bf1.RopeCfg(32)
+    rope = bf1.plan_rope(cfg, DEV)
+    route = bf1.RouteCfg(**DENSE) if dense else bf1.RouteCfg()
+    kp, vp = (torch.full((pages, 64, hkv, d), 0x7f, dtype=torch.uint8, device=DEV).view(E4M3) for _ in range(2))
+    ks, vs = (torch.full((pages, hkv), float("nan"), device=DEV) for _ in range(2))
+    lens = torch.zeros(batch, dtype=torch.int32, device=DEV)
+    table = torch.full((batch, 10), -1, dtype=torch.int32, device=DEV)
+    stack, count = torch.arange(pages, dtype=torch.int32, device=DEV), torch.tensor([pages], dtype=torch.int32, device=DEV)
+    new = torch.tensor([130, 0, 62], dtype=torch.int32, device=DEV)
+    seen = [[], [], []]
+
+    def draw(n):
+        q = torch.randn((n, hq, d), generator=g).to(torch.bfloat16).to(DEV)
+        return q, *(torch.randn((n, hkv, d), generator=g).to(torch.bfloat16).to(DEV) for _ in range(2))
+
+    def keep(k, v, plan):
+        cu = plan.cu_tokens.tolist()
+        turned = bf1.rope_fwd(k, None, plan.positions, rope)[0].double().cpu().numpy()
+        for s in range(batch):
+            for t in range(cu[s], cu[s + 1]):
+                seen[s].append((turned[t], v[t].double().cpu().numpy()))
+
+    # the prompts
+    _, k, v = draw(200)
+    plan = bf1.plan_cache(lens, new, table, pages, 200, stack, count, seqlens_out=lens, free_count_out=count)
+    bf1.cache_write(bf1.rope_fwd(k, None, plan.positions, rope)[0], v, kp, vp, plan, ks, vs)
+    keep(k, v, plan)
+    # the step, captured: its inputs are refilled in place
+    step = bf1.CachePlan.empty(batch, batch, DEV)
+    q, k, v = draw(batch)
+    pages_plan = bf1.plan_decode(lens, table, route)
+    ws = bf1.decode_fp8_workspace(batch, hq, hkv, pages_plan.max_degree, d, DEV)
+    turned, out = torch.zeros_like(q), torch.zeros_like(q)
+    lse = torch.zeros((hq, batch), device=DEV)
+    new.zero_()
+
+    def body():
+        bf1.plan_cache(lens, new, table, pages, batch, stack, count, plan=step, seqlens_out=lens, free_count_out=count)
+        bf1.cache_write(k, v, kp, vp, step, ks, vs, rope=rope, q=q, out_q=turned)
+        bf1.plan_decode(lens, table, route, plan=pages_plan)
+        bf1.decode_fwd_fp8(turned, kp, vp, ks, vs, lens, pages_plan, ws, out=out, lse=lse)
+
+    body()                                                          # adds nothing
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        body()
+    new.fill_(1)
+    for i in range(70):
+        for t, x in zip((q, k, v), draw(batch)):
+            t.copy_(x)
+        graph.replay()
+        keep(k, v, step)
+        assert step.status.item() == 0 and pages_plan.status.item() == 0 and lens.tolist() == [len(x) for x in seen]
+        if i % 10 not in (0, 3):
+            continue
+        for s in range(batch):
+            n = len(seen[s])
+            rows = [r for b in logical(n, dense) for r in range(64 * b, min(64 * b + 64, n))]
+            kk, vv = np.stack([seen[s][r][0] for r in rows]), np.stack([seen[s][r][1] for r in rows])
+            qq = turned[s].double().cpu().numpy()
+            for h in range(hq):
+                key = kk[:, h // 2]
+                x = key @ qq[h] / math.sqrt(d)
+                # a number of the cache is off by 2^-4 of itself, or by 2^-10 of a scale that is below max / 224, twice that where the scale
+                # has grown; the keys seen here have been rounded to bf16 besides
+                off = (np.abs(key) * (2.0 ** -4 + 2.0 ** -7) + np.abs(key).max() / 224 * 2.0 ** -9) @ np.abs(qq[h]) / math.sqrt(d)
+                w = np.exp(x - x.max())
+                val = vv[:, h // 2]
+                o = (w @ val) / w.sum()
+                e = np.expm1(2 * off.max())
+                limit = e * (w @ np.abs(val - o)) / w.sum() * 1.1 + (w @ np.abs(val)) / w.sum() * 2.0 ** -4 * (1 + e) + np.abs(val).max() / 224 * 2.0 ** -9 + 2.0 ** -7 * np.abs(o)
+                assert (np.abs(out[s, h].double().cpu().numpy() - o) <= limit).all()
+                assert abs(lse[h, s].item() - (x.max() + math.log(w.sum()))) <= off.max() + 1e-3
+    # one sequence leaves: its pages come back and its row of the results stays as it is
+    before = count.item()
+    was = out[0].clone()
+    held = (lens[0].item() + 63) // 64
+    new.copy_(torch.tensor([-1, 1, 1], dtype=torch.int32))
+    graph.replay()
+    assert lens[0].item() == 0 and count.item() >= before + held - 2 and torch.equal(out[0], was) and pages_plan.count[0].item() == 0
