@@ -20,8 +20,8 @@
 namespace bf1 {
 
 constexpr int kCachePage = 64;
-constexpr int kTableThreads = 1024;
-constexpr int kTableWarps = kTableThreads / 32;
+constexpr int kTableThreads = 1024;       // at most
+constexpr int kTableHeld = 2048;          // sequences whose starts stand in shared memory; more of them: in bf1_cache_plan::starts
 
 struct TableArgs {
     const int32_t *lens, *add;         // [batch]
@@ -33,48 +33,57 @@ struct TableArgs {
 };
 
 __device__ __forceinline__ int pages_of(int n) { return (n + kCachePage - 1) / kCachePage; }
-
-// Exclusive prefix sums over the CTA of four numbers of every thread at once; `total` gets the sums.  Two barriers.
-__device__ __forceinline__ int4 scan4(int4 v, int4* warp_sums, int4& total) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int4 x = v;
+__device__ __forceinline__ int4 add4(int4 a, int4 b) { return make_int4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
+__device__ __forceinline__ int4 scan_warp(int4 x) {       // inclusive
+    const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
         const int a = __shfl_up_sync(0xffffffffu, x.x, off), b = __shfl_up_sync(0xffffffffu, x.y, off),
                   c = __shfl_up_sync(0xffffffffu, x.z, off), d = __shfl_up_sync(0xffffffffu, x.w, off);
-        if (lane >= off) x.x += a, x.y += b, x.z += c, x.w += d;
+        if (lane >= off) x = add4(x, make_int4(a, b, c, d));
     }
+    return x;
+}
+__device__ __forceinline__ int4 lane4(int4 x, int l) {
+    return make_int4(__shfl_sync(0xffffffffu, x.x, l), __shfl_sync(0xffffffffu, x.y, l), __shfl_sync(0xffffffffu, x.z, l), __shfl_sync(0xffffffffu, x.w, l));
+}
+// Exclusive prefix sums over the CTA of four numbers of every thread at once; `total` gets the sums.
+__device__ __forceinline__ int4 scan4(int4 v, int4* warp_sums, int4& total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int4 x = scan_warp(v);
     __syncthreads();                                     // the last use of warp_sums is over
     if (lane == 31) warp_sums[warp] = x;
     __syncthreads();
-    int4 before = make_int4(0, 0, 0, 0);
-    total = before;
-    for (int w = 0; w < kTableWarps; ++w) {
-        const int4 s = warp_sums[w];
-        if (w < warp) before.x += s.x, before.y += s.y, before.z += s.z, before.w += s.w;
-        total.x += s.x, total.y += s.y, total.z += s.z, total.w += s.w;
-    }
-    return make_int4(before.x + x.x - v.x, before.y + x.y - v.y, before.z + x.z - v.z, before.w + x.w - v.w);
+    const int4 sums = scan_warp(lane < warps ? warp_sums[lane] : make_int4(0, 0, 0, 0));
+    total = lane4(sums, 31);
+    const int4 before = lane4(sums, max(warp - 1, 0));
+    const int4 mine = make_int4(x.x - v.x, x.y - v.y, x.z - v.z, x.w - v.w);
+    return warp ? add4(before, mine) : mine;
 }
 
+// A thread for every sequence first (what each needs, and where it begins, by a scan), then a lane for every unit, which looks up the
+// one page of its tokens.  With few sequences and tokens this is a chain of dependent looks at memory: lengths, stack, page.
 __global__ void __launch_bounds__(kTableThreads, 1) plan_cache_kernel(const TableArgs a) {
-    __shared__ int4 warp_sums[kTableWarps];
+    __shared__ int4 warp_sums[kTableThreads / 32];
+    __shared__ int4 held_starts[kTableHeld];
     __shared__ long long sums[3];
     __shared__ int flags;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
     const int rank = blockIdx.x, ranks = gridDim.x;      // the grid is one cluster
-    const int threads = ranks * kTableThreads, gtid = rank * kTableThreads + tid;
+    const int threads = ranks * blockDim.x, gtid = rank * blockDim.x + tid;
     const bool stack = a.free_pages != nullptr;
     const bf1_cache_plan& p = a.p;
     if (tid < 3) sums[tid] = 0;
     if (tid == 0) flags = 0;
     pdl_wait();
     __syncthreads();
+    const int had = stack ? *a.free_count : 0;
     // ---- what the step needs in all, in 64 bits: it may be refused for any lengths ----------------------------------------------
     long long tokens = 0, fresh = 0, back = 0;
-    int bad = 0;
-    for (int s = tid; s < a.batch; s += kTableThreads) {
+    int bad = 0, n0 = 0, m0 = 0;                          // (n0, m0: of this thread's first sequence, which mostly is its only one)
+    for (int s = tid; s < a.batch; s += blockDim.x) {
         const int n = a.lens[s], m = a.add[s];
+        if (s == tid) n0 = n, m0 = m;
         if (n < 0 || m < -1 || (long long)n + max(m, 0) > (long long)a.max_pages * kCachePage) {
             bad = BF1_DEV_BAD_SEQLENS;
             continue;
@@ -85,64 +94,67 @@ __global__ void __launch_bounds__(kTableThreads, 1) plan_cache_kernel(const Tabl
             else fresh += pages_of(n + m) - pages_of(n);
         }
     }
+    if (warp * 32 < a.batch) {
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-        tokens += __shfl_xor_sync(0xffffffffu, tokens, off);
-        fresh += __shfl_xor_sync(0xffffffffu, fresh, off);
-        back += __shfl_xor_sync(0xffffffffu, back, off);
-        bad |= __shfl_xor_sync(0xffffffffu, bad, off);
-    }
-    if (lane == 0) {
-        atomicAdd(reinterpret_cast<unsigned long long*>(&sums[0]), (unsigned long long)tokens);
-        atomicAdd(reinterpret_cast<unsigned long long*>(&sums[1]), (unsigned long long)fresh);
-        atomicAdd(reinterpret_cast<unsigned long long*>(&sums[2]), (unsigned long long)back);
-        if (bad) atomicOr(&flags, bad);
+        for (int off = 16; off > 0; off >>= 1) {
+            tokens += __shfl_xor_sync(0xffffffffu, tokens, off);
+            fresh += __shfl_xor_sync(0xffffffffu, fresh, off);
+            back += __shfl_xor_sync(0xffffffffu, back, off);
+            bad |= __shfl_xor_sync(0xffffffffu, bad, off);
+        }
+        if (lane == 0) {
+            atomicAdd(reinterpret_cast<unsigned long long*>(&sums[0]), (unsigned long long)tokens);
+            atomicAdd(reinterpret_cast<unsigned long long*>(&sums[1]), (unsigned long long)fresh);
+            atomicAdd(reinterpret_cast<unsigned long long*>(&sums[2]), (unsigned long long)back);
+            if (bad) atomicOr(&flags, bad);
+        }
     }
     __syncthreads();
-    const int had = stack ? *a.free_count : 0;
     int status = flags;
     if (sums[0] > p.capacity_tokens) status |= BF1_DEV_CAPACITY;
     if (stack && (had < 0 || had + sums[2] > a.num_pages || sums[1] > had + sums[2])) status |= BF1_DEV_CAPACITY;
     const bool refused = status != 0;
     const int top = refused ? had : had + (int)sums[2];   // of the stack, with what is put back
     const int total_tokens = refused ? 0 : (int)sums[0];
-    // ---- where every sequence's tokens, pages and units begin --------------------------------------------------------------------
+    // ---- where every sequence's tokens, fresh pages and units begin, and its length: every CTA has them all ------------------------
+    // (a released sequence takes no pages: where its own go on the stack stands there instead)
+    int4* const starts = a.batch <= kTableHeld ? held_starts : reinterpret_cast<int4*>(p.starts);
     int4 at = make_int4(0, 0, 0, 0);                      // tokens, fresh pages, units, pages put back
-    for (int s0 = 0; s0 < a.batch; s0 += kTableThreads) {
+    for (int s0 = 0; s0 < a.batch; s0 += blockDim.x) {
         const int s = s0 + tid;
         int n = 0, m = 0;
         int4 mine = make_int4(0, 0, 0, 0);
-        if (s < a.batch && !refused) {
-            n = a.lens[s];
-            m = a.add[s];
+        if (s < a.batch) {
+            n = s0 ? a.lens[s] : n0;
+            m = refused ? 0 : s0 ? a.add[s] : m0;
             mine.x = max(m, 0);
             mine.y = stack && m > 0 ? pages_of(n + m) - pages_of(n) : 0;
             mine.z = m > 0 ? (n + m - 1) / kCachePage - n / kCachePage + 1 : 0;
             mine.w = stack && m < 0 ? pages_of(n) : 0;
-        } else if (s < a.batch) {
-            n = a.lens[s];
         }
         int4 total;
-        const int4 before = scan4(mine, warp_sums, total);
-        if (s < a.batch && s0 / kTableThreads % ranks == rank) {
-            p.cu_tokens[s] = at.x + before.x;
-            // a released sequence takes no pages: where its own go on the stack stands there instead
-            reinterpret_cast<int4*>(p.starts)[s] = make_int4(at.x + before.x, m < 0 ? at.w + before.w : at.y + before.y, at.z + before.z, n);
+        const int4 before = add4(at, scan4(mine, warp_sums, total));
+        if (s < a.batch) {
+            if (starts == held_starts || s0 / (int)blockDim.x % ranks == rank) starts[s] = make_int4(before.x, m < 0 ? before.w : before.y, before.z, n);
+            if (rank == 0) p.cu_tokens[s] = before.x;
         }
-        at.x += total.x, at.y += total.y, at.z += total.z, at.w += total.w;
-    }
-    if (gtid == 0) {
-        p.cu_tokens[a.batch] = at.x;
-        *p.num_units = at.z;
-        *p.status = status;
+        at = add4(at, total);
     }
     const int units = at.z;
-    cluster_arrive();
-    cluster_wait();                                       // lengths and the count have been read, the starts are there
+    if (gtid == 0) {
+        p.cu_tokens[a.batch] = at.x;
+        *p.num_units = units;
+        *p.status = status;
+    }
+    if (ranks > 1) {                                      // lengths and the count have been read by all: they may be written in place
+        cluster_arrive();
+        cluster_wait();
+    } else {
+        __syncthreads();
+    }
     if (gtid == 0) *p.free_count = top - at.y;
     // ---- lengths after the step; pages put back ------------------------------------------------------------------------------------
-    const int4* starts = reinterpret_cast<const int4*>(p.starts);
-    for (int s0 = (rank * kTableWarps + warp) * 32; s0 < a.batch; s0 += threads) {
+    for (int s0 = (rank * warps + warp) * 32; s0 < a.batch; s0 += threads) {
         const int s = s0 + lane;
         int m = 0, n = 0, to = 0;
         if (s < a.batch) {
@@ -152,21 +164,36 @@ __global__ void __launch_bounds__(kTableThreads, 1) plan_cache_kernel(const Tabl
             to = st.y;
             p.seqlens[s] = m < 0 ? 0 : n + m;
         }
-        unsigned gone = __ballot_sync(0xffffffffu, m < 0 && stack);
-        while (gone) {
-            const int l = __ffs(gone) - 1;
-            gone &= gone - 1;
-            const int count = pages_of(__shfl_sync(0xffffffffu, n, l)), first = had + __shfl_sync(0xffffffffu, to, l);
-            for (int i = lane; i < count; i += 32) a.free_pages[first + i] = a.table[(size_t)(s0 + l) * a.max_pages + i];
+        // fresh pages into the table, where none are put back that might be among them
+        const int held = pages_of(n), want = stack && m > 0 ? pages_of(n + m) - held : 0;
+        if (at.w == 0) {
+            unsigned grown = __ballot_sync(0xffffffffu, want > 1);
+            if (want == 1) a.table[(size_t)s * a.max_pages + held] = a.free_pages[top - 1 - to];
+            while (grown) {
+                const int l = __ffs(grown) - 1;
+                grown &= grown - 1;
+                const int count = __shfl_sync(0xffffffffu, want, l), h = __shfl_sync(0xffffffffu, held, l), f = __shfl_sync(0xffffffffu, to, l);
+                for (int i = lane; i < count; i += 32) a.table[(size_t)(s0 + l) * a.max_pages + h + i] = a.free_pages[top - 1 - (f + i)];
+            }
+        } else {
+            unsigned gone = __ballot_sync(0xffffffffu, m < 0);
+            while (gone) {
+                const int l = __ffs(gone) - 1;
+                gone &= gone - 1;
+                const int count = __shfl_sync(0xffffffffu, held, l), first = had + __shfl_sync(0xffffffffu, to, l);
+                for (int i = lane; i < count; i += 32) a.free_pages[first + i] = a.table[(size_t)(s0 + l) * a.max_pages + i];
+            }
         }
     }
     if (at.w > 0) {                                       // (the same in every CTA)
-        cluster_arrive();
-        cluster_wait();
-    }
-    // ---- fresh pages into the table ------------------------------------------------------------------------------------------------
-    if (at.y > 0) {
-        for (int s0 = (rank * kTableWarps + warp) * 32; s0 < a.batch; s0 += threads) {
+        if (ranks > 1) {
+            cluster_arrive();
+            cluster_wait();
+        } else {
+            __syncthreads();
+        }
+        // fresh pages, some of them from what has just been put back, page by page: warps take 32 sequences each
+        for (int s0 = (rank * warps + warp) * 32; s0 < a.batch; s0 += threads) {
             const int s = s0 + lane;
             int held = 0, want = 0, first = 0;
             if (s < a.batch) {
@@ -185,52 +212,54 @@ __global__ void __launch_bounds__(kTableThreads, 1) plan_cache_kernel(const Tabl
             }
         }
     }
-    // ---- positions, slots and units, four tokens to a thread -------------------------------------------------------------------------
-    for (int t0 = gtid * 4; t0 < p.capacity_tokens; t0 += threads * 4) {
-        int s = 0;
-        int4 st = make_int4(0, 0, 0, 0);
-        int end = 0;
-        if (t0 < total_tokens) {                          // the last sequence that begins at or in front of t0
-            int lo = 0, hi = a.batch;
+    // ---- units, a lane to each, then their tokens' positions and slots --------------------------------------------------------------
+    for (int u0 = (rank * warps + warp) * 32; u0 < units; u0 += threads) {
+        const int u = u0 + lane;
+        int t = 0, count = 0, pos = 0, slot = -1;
+        if (u < units) {
+            int lo = 0, hi = a.batch;                     // the last sequence that begins at or in front of unit u
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
-                if (starts[mid].x <= t0) lo = mid;
+                if (starts[mid].z <= u) lo = mid;
                 else hi = mid;
             }
-            s = lo;
-            st = starts[s];
-            end = s + 1 < a.batch ? starts[s + 1].x : total_tokens;
-        }
-        for (int i = 0; i < 4 && t0 + i < p.capacity_tokens; ++i) {
-            const int t = t0 + i;
-            int pos = -1, slot = -1;
-            if (t < total_tokens) {
-                while (t >= end) {                        // (every token below the total belongs to some sequence)
-                    ++s;
-                    st = starts[s];
-                    end = s + 1 < a.batch ? starts[s + 1].x : total_tokens;
-                }
-                pos = st.w + (t - st.x);
-                const int lp = pos / kCachePage, row = pos % kCachePage, held = pages_of(st.w);
-                int page = stack && lp >= held ? a.free_pages[top - 1 - (st.y + lp - held)] : a.table[(size_t)s * a.max_pages + lp];
-                if (page < 0 || page >= a.num_pages) {
-                    atomicOr(p.status, BF1_DEV_BAD_ROUTE);
-                    page = -1;
-                } else {
-                    slot = page * kCachePage + row;
-                }
-                if (t == st.x || row == 0) {              // the first token of a unit
-                    const int u = st.z + lp - st.w / kCachePage;
-                    if (u < p.capacity_units) reinterpret_cast<int4*>(p.units)[u] = make_int4(t, min(kCachePage - row, end - t), page, row);
-                }
+            const int4 st = starts[lo];
+            const int end = lo + 1 < a.batch ? starts[lo + 1].x : total_tokens;
+            const int lp = st.w / kCachePage + (u - st.z), held = pages_of(st.w);
+            pos = max(st.w, lp * kCachePage);
+            t = st.x + (pos - st.w);
+            const int row = pos % kCachePage;
+            count = min(kCachePage - row, end - t);
+            int page = stack && lp >= held ? a.free_pages[top - 1 - (st.y + lp - held)] : a.table[(size_t)lo * a.max_pages + lp];
+            if (page < 0 || page >= a.num_pages) {
+                atomicOr(p.status, BF1_DEV_BAD_ROUTE);
+                page = -1;
+            } else {
+                slot = page * kCachePage + row;
             }
-            p.positions[t] = pos;
+            if (u < p.capacity_units) reinterpret_cast<int4*>(p.units)[u] = make_int4(t, count, page, row);
+            p.positions[t] = pos;                         // (single tokens, side by side in a step of them)
             p.slots[t] = slot;
         }
+        unsigned more = __ballot_sync(0xffffffffu, count > 1);
+        while (more) {
+            const int l = __ffs(more) - 1;
+            more &= more - 1;
+            const int tl = __shfl_sync(0xffffffffu, t, l), cl = __shfl_sync(0xffffffffu, count, l), pl = __shfl_sync(0xffffffffu, pos, l),
+                      sl = __shfl_sync(0xffffffffu, slot, l);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int k = 1 + lane + 32 * i;
+                if (k < cl) {
+                    p.positions[tl + k] = pl + k;
+                    p.slots[tl + k] = sl < 0 ? -1 : sl + k;
+                }
+            }
+        }
     }
+    for (int t = total_tokens + gtid; t < p.capacity_tokens; t += threads) p.positions[t] = p.slots[t] = -1;
     for (int u = units + gtid; u < p.capacity_units; u += threads) reinterpret_cast<int4*>(p.units)[u] = make_int4(-1, -1, -1, -1);
 }
-
 
 // ---- keys and values into the pages ------------------------------------------------------------------------------------------------
 
@@ -239,11 +268,11 @@ struct WriteArgs {
     Rows q, out_q;
     uint8_t* pages[2];                 // [num_pages, 64, hkv, D], bf16 or e4m3
     float* scales[2];                  // [num_pages, hkv] (8 bits)
-    const int4* units;
-    const int32_t *num_units, *positions;
+    const int4* units;                 // [num_units], those behind the last one with -1 tokens
+    const int32_t* positions;
     int32_t* status;
-    RopeTable rope;                    // dim 0: nothing is rotated
-    int32_t tokens, hq, hkv, num_pages, capacity_units;
+    RopeTable rope;
+    int32_t tokens, hq, hkv, num_pages, num_units;
     int64_t write_ctas;                // CTAs behind them rotate queries
     int32_t q_shares;                  // shares of the query heads
 };
@@ -270,6 +299,14 @@ __device__ __forceinline__ float magnitude_of(const float (&x)[8], float top) {
     }
     return top;
 }
+// The same on eight bf16 values, as whole numbers, two at a time: without their sign they are ordered as their bits are, an infinity
+// above every finite value and NaN above that.  Both halves of `top` run for themselves.
+__device__ __forceinline__ uint32_t magnitude_bits(const uint4& v, uint32_t top) {
+    top = __vmaxu2(top, v.x & 0x7fff7fffu);
+    top = __vmaxu2(top, v.y & 0x7fff7fffu);
+    top = __vmaxu2(top, v.z & 0x7fff7fffu);
+    return __vmaxu2(top, v.w & 0x7fff7fffu);
+}
 // The smallest power of two, 2^-64 at least, under which `top` is within 448 = 1.75 * 2^8.
 __device__ __forceinline__ float scale_for(float top) {
     const int e = (int)((__float_as_uint(top) + 0x1fffffu) >> 23) - 8;     // above 1.75 the sum carries into the exponent
@@ -284,6 +321,20 @@ __device__ __forceinline__ uint2 quantize(const float (&x)[8], float inv) {   //
 __device__ __forceinline__ uint2 requantize(uint2 v, float ratio) {
     const float2 a = from_e4m3x2(v.x & 0xffffu), b = from_e4m3x2(v.x >> 16), c = from_e4m3x2(v.y & 0xffffu), d = from_e4m3x2(v.y >> 16);
     return make_uint2(e4m3x4(a.x * ratio, a.y * ratio, b.x * ratio, b.y * ratio), e4m3x4(c.x * ratio, c.y * ratio, d.x * ratio, d.y * ratio));
+}
+
+__device__ __forceinline__ uint2 quantize_finite(const float (&x)[8], float inv) {
+    return make_uint2(e4m3x4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv), e4m3x4(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv));
+}
+// The rows in front of a unit's own under the page's new scale, and that scale.  `out`: this thread's chunk of row 0.
+template <int kRows>
+__device__ __forceinline__ void finish_page(uint8_t* out, size_t pitch, int r0, int rows, float before, float scale, float* at) {
+    if (rows > 0 && before != scale)
+        for (int r = r0; r < rows; r += kRows) {
+            uint2* v = reinterpret_cast<uint2*>(out + r * pitch);
+            *v = requantize(*v, before * (1.f / scale));
+        }
+    if (threadIdx.x == 0) *at = scale;
 }
 
 // A unit whose tokens, rows and page exist.  What a plan holds is looked at once more here: a plan for other tensors than these, or one
@@ -304,76 +355,125 @@ __device__ __forceinline__ void rotate_queries(const WriteArgs& a) {
     rope_heads<4>(a.rope, position, token, threadIdx.x % kPerToken, 1.f, a.q, a.q, a.out_q, a.out_q, a.hq, a.hq, (int)(block % a.q_shares), a.q_shares);
 }
 
-// A CTA per unit, KV head and K or V: the rows stay in registers between the look for their largest value and the store.
-template <int D, bool kFp8>
+// A CTA per unit, KV head and K or V: the rows stay in registers between the look for their largest value and the store, as they
+// came where nothing is rotated (32 registers a thread instead of 64).
+template <int D, bool kFp8, bool kRope>
 __global__ void __launch_bounds__(128) cache_write_pages_kernel(const WriteArgs a) {
     constexpr int kChunks = D / 8, kRows = 128 / kChunks, kPer = kCachePage / kRows;
-    __shared__ float warp_top[4];
+    __shared__ uint32_t warp_top[4];
     pdl_wait();
-    if ((int64_t)blockIdx.x >= a.write_ctas) return rotate_queries<D>(a);
+    if (kRope && (int64_t)blockIdx.x >= a.write_ctas) return rotate_queries<D>(a);
     const int which = blockIdx.x & 1, h = (blockIdx.x >> 1) % a.hkv, unit = (blockIdx.x >> 1) / a.hkv;
-    if (unit >= *a.num_units) return;
     const int4 u = a.units[unit];
+    if (u.y < 0) return;                                 // behind the last unit
     if (!unit_ok(a, u)) {
         if (threadIdx.x == 0) atomicOr(a.status, BF1_DEV_BAD_ROUTE);
         return;
     }
+    float* const at = kFp8 ? a.scales[which] + (size_t)u.z * a.hkv + h : nullptr;
+    const float before = kFp8 && u.w > 0 ? *at : 0.f;
     const int c = threadIdx.x % kChunks, r0 = threadIdx.x / kChunks;
     const Rows& in = a.x[which];
-    float x[kPer][8], top = 0.f;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const int r = r0 + i * kRows;
-        if (r < u.y) {
-            const __nv_bfloat16* row = in.at((int64_t)u.x + r, h);
-            if (which == 0 && a.rope.dim) rope_chunk(a.rope, a.positions[u.x + r], row, c, x[i]);
-            else unpack_bf16x8(*reinterpret_cast<const uint4*>(row + 8 * c), x[i]);
-            top = magnitude_of(x[i], top);
-        }
-    }
     const size_t pitch = (size_t)a.hkv * D;
     const size_t first = ((size_t)u.z * kCachePage) * pitch + (size_t)h * D + 8 * c;     // element of the page's row 0
-    if constexpr (!kFp8) {
-        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.pages[which]) + first;
+    if (!kRope || which == 1) {
+        uint4 x[kPer];
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int r = r0 + i * kRows;
-            if (r < u.y) *reinterpret_cast<uint4*>(out + (u.w + r) * pitch) = pack_bf16x8(x[i]);
+            x[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (r < u.y) x[i] = *reinterpret_cast<const uint4*>(in.at((int64_t)u.x + r, h) + 8 * c);
+        }
+        if constexpr (!kFp8) {
+            __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.pages[which]) + first;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const int r = r0 + i * kRows;
+                if (r < u.y) *reinterpret_cast<uint4*>(out + (u.w + r) * pitch) = x[i];
+            }
+        } else {
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) top = magnitude_bits(x[i], top);
+            top = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));
+            if ((threadIdx.x & 31) == 0) warp_top[threadIdx.x >> 5] = top;
+            __syncthreads();
+            top = max(max(warp_top[0], warp_top[1]), max(warp_top[2], warp_top[3]));
+            if (top >= 0x7f80u) {                        // not all finite: once more without those (the whole CTA)
+                float most = 0.f;
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) {
+                    float y[8];
+                    unpack_bf16x8(x[i], y);
+                    most = magnitude_of(y, most);
+                }
+                __syncthreads();
+                top = __reduce_max_sync(0xffffffffu, __float_as_uint(most) >> 16);
+                if ((threadIdx.x & 31) == 0) warp_top[threadIdx.x >> 5] = top;
+                __syncthreads();
+                top = max(max(warp_top[0], warp_top[1]), max(warp_top[2], warp_top[3])) | 0x80000000u;
+            }
+            const bool finite = (top >> 31) == 0;
+            const float scale = fmaxf(scale_for(__uint_as_float(top << 16)), before), inv = 1.f / scale;
+            uint8_t* out = a.pages[which] + first;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const int r = r0 + i * kRows;
+                if (r < u.y) {
+                    float y[8];
+                    unpack_bf16x8(x[i], y);
+                    *reinterpret_cast<uint2*>(out + (u.w + r) * pitch) = finite ? quantize_finite(y, inv) : quantize(y, inv);
+                }
+            }
+            finish_page<kRows>(out, pitch, r0, u.w, before, scale, at);
         }
         return;
     }
-    float* const at = a.scales[which] + (size_t)u.z * a.hkv + h;
-    const float before = u.w > 0 ? *at : 0.f;
+    if constexpr (kRope) {
+        float x[kPer][8], top = 0.f;
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-    if ((threadIdx.x & 31) == 0) warp_top[threadIdx.x >> 5] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(warp_top[0], warp_top[1]), fmaxf(warp_top[2], warp_top[3]));
-    const float scale = fmaxf(scale_for(top), before), inv = 1.f / scale;
-    uint8_t* out = a.pages[which] + first;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const int r = r0 + i * kRows;
-        if (r < u.y) *reinterpret_cast<uint2*>(out + (u.w + r) * pitch) = quantize(x[i], inv);
-    }
-    if (u.w > 0 && before != scale)
-        for (int r = r0; r < u.w; r += kRows) {
-            uint2* v = reinterpret_cast<uint2*>(out + r * pitch);
-            *v = requantize(*v, before * inv);
+        for (int i = 0; i < kPer; ++i) {
+            const int r = r0 + i * kRows;
+            if (r < u.y) {
+                rope_chunk(a.rope, a.positions[u.x + r], in.at((int64_t)u.x + r, h), c, x[i]);
+                top = magnitude_of(x[i], top);
+            }
         }
-    if (threadIdx.x == 0) *at = scale;
+        if constexpr (!kFp8) {
+            __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.pages[which]) + first;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const int r = r0 + i * kRows;
+                if (r < u.y) *reinterpret_cast<uint4*>(out + (u.w + r) * pitch) = pack_bf16x8(x[i]);
+            }
+        } else {
+            const uint32_t bits = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
+            if ((threadIdx.x & 31) == 0) warp_top[threadIdx.x >> 5] = bits;
+            __syncthreads();
+            top = __uint_as_float(max(max(warp_top[0], warp_top[1]), max(warp_top[2], warp_top[3])));
+            const float scale = fmaxf(scale_for(top), before), inv = 1.f / scale;
+            uint8_t* out = a.pages[which] + first;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const int r = r0 + i * kRows;
+                if (r < u.y) *reinterpret_cast<uint2*>(out + (u.w + r) * pitch) = quantize(x[i], inv);
+            }
+            finish_page<kRows>(out, pitch, r0, u.w, before, scale, at);
+        }
+    }
 }
 
 // A warp per unit and KV head, half of it for K and half for V: for units of a token or a few, which a CTA would not fill.
-template <int D, bool kFp8>
+template <int D, bool kFp8, bool kRope>
 __global__ void __launch_bounds__(128) cache_write_tokens_kernel(const WriteArgs a) {
     constexpr int kChunks = D / 8, kRows = 16 / kChunks;        // lanes to a row, rows at a time
     pdl_wait();
-    if ((int64_t)blockIdx.x >= a.write_ctas) return rotate_queries<D>(a);
+    if (kRope && (int64_t)blockIdx.x >= a.write_ctas) return rotate_queries<D>(a);
     const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
     const int unit = (int)(item / a.hkv), h = (int)(item % a.hkv);
-    if (unit >= min(*a.num_units, a.capacity_units)) return;    // (the last CTA may have warps to spare)
+    if (unit >= a.num_units) return;                            // (the last CTA may have warps to spare)
     const int4 u = a.units[unit];
+    if (u.y < 0) return;                                        // behind the last unit
     const int lane = threadIdx.x & 31, which = lane >> 4, c = lane % kChunks, r0 = (lane & 15) / kChunks;
     if (!unit_ok(a, u)) {
         if (lane == 0) atomicOr(a.status, BF1_DEV_BAD_ROUTE);
@@ -382,7 +482,7 @@ __global__ void __launch_bounds__(128) cache_write_tokens_kernel(const WriteArgs
     const Rows& in = a.x[which];
     auto load = [&](int r, float (&x)[8]) {
         const __nv_bfloat16* row = in.at((int64_t)u.x + r, h);
-        if (which == 0 && a.rope.dim) rope_chunk(a.rope, a.positions[u.x + r], row, c, x);
+        if (kRope && which == 0) rope_chunk(a.rope, a.positions[u.x + r], row, c, x);
         else unpack_bf16x8(*reinterpret_cast<const uint4*>(row + 8 * c), x);
     };
     const size_t pitch = (size_t)a.hkv * D;
@@ -469,8 +569,10 @@ extern "C" int bf1_plan_cache(const int32_t* seqlens_dev, const int32_t* new_len
     a.max_pages = max_pages_per_seq;
     a.num_pages = num_pages;
     a.p = *out;
-    const int ctas = out->capacity_tokens <= 4096 ? 1 : 8;
-    BF1_CUDA_CHECK(launch_pdl_cluster(plan_cache_kernel, dim3(ctas), dim3(ctas), kTableThreads, 0, (cudaStream_t)stream, a));
+    // one CTA for what 1024 threads do in a few rounds
+    const int ctas = out->capacity_tokens <= 8192 && out->batch <= kTableThreads ? 1 : 8;
+    const int threads = ctas == 1 && out->batch <= 128 && out->capacity_tokens <= 512 ? 128 : kTableThreads;
+    BF1_CUDA_CHECK(launch_pdl_cluster(plan_cache_kernel, dim3(ctas), dim3(ctas), threads, 0, (cudaStream_t)stream, a));
     return BF1_OK;
 }
 
@@ -505,7 +607,6 @@ extern "C" int bf1_cache_write(const bf1_rows* k, const bf1_rows* v, const bf1_r
     a.scales[0] = k_scales;
     a.scales[1] = v_scales;
     a.units = reinterpret_cast<const int4*>(plan->units);
-    a.num_units = plan->num_units;
     a.positions = plan->positions;
     a.status = plan->status;
     a.rope = rope ? table_of(rope) : RopeTable{nullptr, 0, 0, 1.f};
@@ -513,18 +614,20 @@ extern "C" int bf1_cache_write(const bf1_rows* k, const bf1_rows* v, const bf1_r
     a.hq = hq;
     a.hkv = hkv;
     a.num_pages = num_pages;
-    a.capacity_units = plan->capacity_units;
-    static const WriteKernel kernels[2][2][2] = {   // [few tokens to a unit][8 bits][d = 128]
-        {{cache_write_pages_kernel<64, false>, cache_write_pages_kernel<128, false>}, {cache_write_pages_kernel<64, true>, cache_write_pages_kernel<128, true>}},
-        {{cache_write_tokens_kernel<64, false>, cache_write_tokens_kernel<128, false>}, {cache_write_tokens_kernel<64, true>, cache_write_tokens_kernel<128, true>}}};
+#define BF1_WRITE(kernel, rope) {{kernel<64, false, rope>, kernel<128, false, rope>}, {kernel<64, true, rope>, kernel<128, true, rope>}}
+    static const WriteKernel kernels[2][2][2][2] = {   // [few tokens to a unit][a rope][8 bits][d = 128]
+        {BF1_WRITE(cache_write_pages_kernel, false), BF1_WRITE(cache_write_pages_kernel, true)},
+        {BF1_WRITE(cache_write_tokens_kernel, false), BF1_WRITE(cache_write_tokens_kernel, true)}};
+#undef BF1_WRITE
     const bool few = tokens < 8 * (int64_t)plan->batch;
     const int64_t units = bf1_cache_plan_units(plan->batch, tokens);
     if (plan->capacity_units < units) return fail(BF1_ERR_CAPACITY, "cache plan capacity_units %d < %d", plan->capacity_units, (int)units);
+    a.num_units = (int32_t)units;
     a.write_ctas = few ? (units * hkv + 3) / 4 : units * hkv * 2;
     const int64_t token_ctas = ((int64_t)tokens + 128 / (d / 16) - 1) / (128 / (d / 16));
     a.q_shares = hq ? (int)std::max<int64_t>(1, std::min<int64_t>(hq, 148 * 8 / token_ctas)) : 0;
     const int64_t ctas = a.write_ctas + token_ctas * a.q_shares;
     if (ctas > 0x7fffffffLL) return fail(BF1_ERR_UNSUPPORTED, "%d tokens of %d query and %d KV heads in one call", tokens, hq, hkv);
-    BF1_CUDA_CHECK(launch_pdl(kernels[few][k_scales != nullptr][d == 128], dim3((unsigned)ctas), 128, 0, (cudaStream_t)stream, a));
+    BF1_CUDA_CHECK(launch_pdl(kernels[few][rope != nullptr][k_scales != nullptr][d == 128], dim3((unsigned)ctas), 128, 0, (cudaStream_t)stream, a));
     return BF1_OK;
 }
