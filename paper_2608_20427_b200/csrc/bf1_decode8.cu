@@ -29,6 +29,11 @@ constexpr int kD8Consumers = 128, kD8Threads = kD8Consumers + 32;
 constexpr int kD8MaxStages = 8;
 constexpr int kD8MaxScan = 1024;         // sequences whose lists are cut (more of them: a CTA per list)
 constexpr int kD8MaxRuns = 640;          // runs at most, which is what the workspace has room for
+constexpr int kD8MaxCtas = 16;           // to a cluster
+constexpr int kD8Held = 64;              // pages of a list that the copying warp holds at once
+
+// How the lists are dealt: kRuns as above; kWhole a CTA per list; kParts a cluster per list, each CTA an even part of it.
+enum { kRuns, kWhole, kParts };
 
 struct Decode8Args {
     const __nv_bfloat16* q;              // [batch, hq, d]
@@ -39,8 +44,9 @@ struct Decode8Args {
     float scale_log2;
     __nv_bfloat16* o;                    // [batch, hq, d]
     float* lse;                          // [hq, batch]
-    int32_t runs;                        // per KV head; 0: a CTA per list
-    int32_t stages;
+    int32_t runs;                        // kRuns: per KV head
+    int32_t stages;                      // pages in a CTA's ring
+    int32_t nctas, share;                // kParts: CTAs to a list, columns (of the heads' G d) that each adds up, a multiple of 32
     int32_t* bases;                      // workspace: [batch + 1] pages in front of every list
     float2* part_ml;                     // [hkv][runs][2][group] (max, sum) ...
     float* part_o;                       // [hkv][runs][2][group][d] ... and sum of a cut list's part
@@ -205,8 +211,8 @@ struct Merge8 {                          // the four warps' states at the end of
     float o[4][kHeads][D + 4], m[4][kHeads], l[4][kHeads];
 };
 
-// grid (hkv, runs), or (hkv, batch) with runs = 0
-template <int D, int kHeads>
+// grid (hkv, runs), (hkv, batch) or (hkv, batch, CTAs of the cluster)
+template <int D, int kHeads, int kMode>
 __global__ void __launch_bounds__(kD8Threads, 3) decode8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                                                                 const Decode8Args a) {
     constexpr int kPageBytes = kP8 * D;
@@ -217,13 +223,15 @@ __global__ void __launch_bounds__(kD8Threads, 3) decode8_kernel(const __grid_con
     __shared__ int warp_sums[kD8Threads / 32];
     __shared__ int abort_flag;
     const uint32_t ring = (smem_u32(dsmem) + 1023) & ~1023u;
-    int* const bases = reinterpret_cast<int*>(dsmem + (ring - smem_u32(dsmem)) + (size_t)a.stages * 2 * kPageBytes);
+    uint8_t* const behind = dsmem + (ring - smem_u32(dsmem)) + (size_t)a.stages * 2 * kPageBytes;
+    int* const bases = reinterpret_cast<int*>(behind);                 // kRuns
+    const uint32_t sums_at = smem_u32(behind), gather_at = sums_at + (a.nctas * kHeads * 8 + 15) / 16 * 16;   // kParts: [CTA][head] (max, sum), [CTA][share] columns
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, kvh = blockIdx.x;
     const uint32_t full = smem_u32(bars), empty = full + 8 * kD8MaxStages;
     if (tid == 0) {
         abort_flag = 0;
         for (int i = 0; i < a.stages; ++i) {
-            mbar_init(full + 8 * i, 1);
+            mbar_init(full + 8 * i, 2);                               // the copies, the scales
             mbar_init(empty + 8 * i, kD8Consumers / 32);
         }
         fence_mbar_init();
@@ -231,31 +239,35 @@ __global__ void __launch_bounds__(kD8Threads, 3) decode8_kernel(const __grid_con
         tma_prefetch_desc(&tm_v);
     }
     pdl_wait();
-    // ---- the pages in front of every list ------------------------------------------------------------------------------------------
-    auto pages_of_list = [&](int s) {
+    const bool reports = kvh == 0 && tid == 0 && (kMode == kParts ? blockIdx.z == 0 : true);
+    auto pages_of_list = [&](int s, bool report) {
         const int n = a.seqlens[s];
         const int c = max(min(a.count[s], a.max_degree), 0);
         if (c > 0 && (n < 1 || (n - 1) / kP8 != a.block[s])) {       // the plan belongs to another 64 tokens
-            if (kvh == 0 && (a.runs == 0 || blockIdx.y == 0)) atomicOr(a.status, BF1_DEV_BAD_ROUTE);
+            if (report) atomicOr(a.status, BF1_DEV_BAD_ROUTE);
             return 0;
         }
         return c;
     };
-    int s = 0, x0 = 0, x1 = 0;
-    if (a.runs == 0) {
+    // ---- this CTA's pages: x0 .. x1 - 1 of the row (kRuns), or of its list -------------------------------------------------------------
+    int s = 0, x0 = 0, x1 = 0, count = 0, held[2] = {-1, -1};
+    if constexpr (kMode != kRuns) {
         s = blockIdx.y;
-        if (tid == 0) {
-            const int c = pages_of_list(s);
-            bases[0] = 0;
-            bases[1] = c;
-        }
-        __syncthreads();
-        x1 = bases[1];
+        if (warp == kD8Consumers / 32)                               // the list is asked for together with its length
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (lane + 32 * i < a.max_degree) held[i] = a.page[(size_t)s * a.max_degree + lane + 32 * i];
+        count = pages_of_list(s, reports);
+        x0 = kMode == kParts ? blockIdx.z * count / a.nctas : 0;
+        x1 = kMode == kParts ? (blockIdx.z + 1) * count / a.nctas : count;
+        if (kMode == kWhole && count == 0) return;
+        __syncthreads();                                             // the barriers are there
+        if constexpr (kMode == kParts) cluster_arrive_relaxed();     // (waited for in front of the first store to another CTA)
     } else {
         const int per = (a.batch + kD8Threads - 1) / kD8Threads, lo = min(tid * per, a.batch), hi = min(lo + per, a.batch);
         int sum = 0;
         for (int i = lo; i < hi; ++i) {
-            const int c = pages_of_list(i);
+            const int c = pages_of_list(i, kvh == 0 && blockIdx.y == 0);
             bases[i] = c;
             sum += c;
         }
@@ -284,10 +296,11 @@ __global__ void __launch_bounds__(kD8Threads, 3) decode8_kernel(const __grid_con
         }
         if (kvh == 0 && blockIdx.y == 0)
             for (int i = tid; i <= a.batch; i += kD8Threads) a.bases[i] = bases[i];
+        if (x0 >= x1) return;
     }
-    if (x0 >= x1) return;
     // the list that page x belongs to
     auto list_of = [&](int x) {
+        if constexpr (kMode != kRuns) return s;
         int lo = 0, hi = a.batch;
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
@@ -297,40 +310,58 @@ __global__ void __launch_bounds__(kD8Threads, 3) decode8_kernel(const __grid_con
         return lo;
     };
     if (warp == kD8Consumers / 32) {
-        // ---- the copying warp: a lane looks up a page and its scales, 32 pages ahead of their use -------------------------------------
-        auto look_up = [&](int x, int& pg, float2& sc) {
-            pg = 0;
-            sc = make_float2(0.f, 0.f);
-            if (x >= x1) return;
-            const int sx = a.runs == 0 ? s : list_of(x);
-            pg = a.page[(size_t)sx * a.max_degree + (x - (a.runs == 0 ? 0 : bases[sx]))];
+        // ---- the copying warp: a lane looks up a page, 32 pages ahead of their use -----------------------------------------------------
+        auto look_up = [&](int x) {
+            int pg = 0;
+            if constexpr (kMode != kRuns) {
+                const int h0 = __shfl_sync(0xffffffffu, held[0], x & 31), h1 = __shfl_sync(0xffffffffu, held[1], x & 31);
+                pg = x < 32 ? h0 : h1;
+            }
+            if (x >= x1) return 0;
+            if (kMode == kRuns || x >= kD8Held) {
+                const int sx = list_of(x);
+                pg = a.page[(size_t)sx * a.max_degree + (kMode == kRuns ? x - bases[sx] : x)];
+            }
             if (pg < 0 || pg >= a.num_pages) {
                 atomicOr(a.status, BF1_DEV_BAD_ROUTE);
                 pg = 0;
             }
-            sc = make_float2(a.k_scales[(size_t)pg * a.hkv + kvh], a.v_scales[(size_t)pg * a.hkv + kvh]);
+            return pg;
         };
-        int pg, stage = 0, parity = 1, issued = 0;
+        auto scales_of = [&](int x, int pg) {
+            return x < x1 ? make_float2(a.k_scales[(size_t)pg * a.hkv + kvh], a.v_scales[(size_t)pg * a.hkv + kvh]) : make_float2(0.f, 0.f);
+        };
+        auto copy = [&](int to_stage, int pg) {
+            const uint32_t bar = full + 8 * to_stage, to = ring + to_stage * 2 * kPageBytes;
+            mbar_expect_tx(bar, 2 * kPageBytes);
+            tma_load_3d(to, &tm_k, 0, kvh, pg * kP8, bar);
+            tma_load_3d(to + kPageBytes, &tm_v, 0, kvh, pg * kP8, bar);
+        };
+        int pg = look_up(x0 + lane), stage = 0, parity = 1, issued = 0;
+        // the ring is empty: its first pages are asked for while the scales are still being fetched
+        const int ahead = min(x1 - x0, a.stages);
+        for (int i = 0; i < ahead; ++i) {
+            const int p = __shfl_sync(0xffffffffu, pg, i);
+            if (elect_one()) copy(i, p);
+            __syncwarp();
+        }
+        float2 sc = scales_of(x0 + lane, pg);
         bool ok = true;
-        float2 sc;
-        look_up(x0 + lane, pg, sc);
         for (int xb = x0; xb < x1 && ok; xb += 32) {
-            int pg_next;
-            float2 sc_next;
-            look_up(xb + 32 + lane, pg_next, sc_next);
+            const int pg_next = look_up(xb + 32 + lane);
+            const float2 sc_next = scales_of(xb + 32 + lane, pg_next);
             const int n = min(32, x1 - xb);
             for (int i = 0; i < n; ++i) {
                 const int p = __shfl_sync(0xffffffffu, pg, i);
                 const float2 ps = make_float2(__shfl_sync(0xffffffffu, sc.x, i), __shfl_sync(0xffffffffu, sc.y, i));
-                // (a barrier that has not completed a phase lets a wait for parity 1 pass: the ring is empty at first)
-                ok = __all_sync(0xffffffffu, mbar_wait(empty + 8 * stage, parity, &abort_flag, a.status));
-                if (!ok) break;
+                if (issued >= a.stages) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(empty + 8 * stage, parity, &abort_flag, a.status));
+                    if (!ok) break;
+                }
                 if (lane == 0) {
-                    const uint32_t bar = full + 8 * stage, to = ring + stage * 2 * kPageBytes;
+                    if (issued >= a.stages) copy(stage, p);
                     page_scales[stage] = ps;
-                    mbar_expect_tx(bar, 2 * kPageBytes);
-                    tma_load_3d(to, &tm_k, 0, kvh, p * kP8, bar);
-                    tma_load_3d(to + kPageBytes, &tm_v, 0, kvh, p * kP8, bar);
+                    mbar_arrive(full + 8 * stage);
                 }
                 __syncwarp();
                 ++issued;
@@ -345,17 +376,22 @@ __global__ void __launch_bounds__(kD8Threads, 3) decode8_kernel(const __grid_con
                 while (!mbar_try_wait(full + 8 * (i % a.stages), i / a.stages & 1) && clock64() - t0 < kWaitCycles) {
                 }
         }
+        if constexpr (kMode == kParts) {                     // (the whole CTA arrives at the cluster's barriers)
+            __syncwarp();
+            cluster_wait();
+            cluster_arrive();
+            cluster_wait();
+        }
         return;
     }
     // ---- the four warps that compute: one list, or the part of it that lies in this run, after the other ----------------------------------
     const int key0 = warp * 16, hbase = kvh * a.group, gid = lane >> 2, tig = lane & 3;
+    constexpr int kCols = kHeads * D / kD8Consumers, kPerHead = kD8Consumers / kHeads;
+    const int h = tid / kPerHead, c0 = tid % kPerHead * kCols;
     int stage = 0, parity = 0;
-    if (a.runs != 0) s = list_of(x0);
-    for (int x = x0; x < x1;) {
-        if (a.runs != 0)
-            while (bases[s + 1] <= x) ++s;                   // (empty lists)
-        const int first = a.runs == 0 ? 0 : bases[s], last = a.runs == 0 ? x1 : bases[s + 1], end = min(x1, last);
-        const bool head = x == first, whole = head && end == last;
+    s = list_of(x0);
+    // the part of list s from page x to `end` (of `last`), and the four warps' states merged: (max, sum) and this thread's columns
+    auto part = [&](int x, int end, int last, float& m, float& l, float (&out)[kCols]) {
         const int n = a.seqlens[s], tail = n - (n - 1) / kP8 * kP8;
         uint32_t qb[D / 16][2];
         float f[2];
@@ -372,84 +408,181 @@ __global__ void __launch_bounds__(kD8Threads, 3) decode8_kernel(const __grid_con
             if (++stage == a.stages) stage = 0, parity ^= 1;
         }
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int off = 4; off < 32; off <<= 1) w.l[h] += __shfl_xor_sync(0xffffffffu, w.l[h], off);
+            for (int off = 4; off < 32; off <<= 1) w.l[i] += __shfl_xor_sync(0xffffffffu, w.l[i], off);
         if (2 * tig < kHeads) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int i = 0; i < 2; ++i) {
                 if (gid == 0) {
-                    st.m[warp][2 * tig + h] = w.m[h];
-                    st.l[warp][2 * tig + h] = w.l[h];
+                    st.m[warp][2 * tig + i] = w.m[i];
+                    st.l[warp][2 * tig + i] = w.l[i];
                 }
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c)
-                    *reinterpret_cast<float2*>(&st.o[warp][2 * tig + h][16 * c + 2 * gid]) = make_float2(w.acc[c][h], w.acc[c][2 + h]);
+                    *reinterpret_cast<float2*>(&st.o[warp][2 * tig + i][16 * c + 2 * gid]) = make_float2(w.acc[c][i], w.acc[c][2 + i]);
             }
         }
         consumers_sync();
-        constexpr int kCols = kHeads * D / kD8Consumers, kPerHead = kD8Consumers / kHeads;
-        const int h = tid / kPerHead, c0 = tid % kPerHead * kCols;
-        if (h < a.group) {
-            const float m = fmaxf(fmaxf(st.m[0][h], st.m[1][h]), fmaxf(st.m[2][h], st.m[3][h]));
-            const float base = m == -INFINITY ? 0.f : m;
-            float l = 0.f, out[kCols] = {};
+        m = fmaxf(fmaxf(st.m[0][h], st.m[1][h]), fmaxf(st.m[2][h], st.m[3][h]));
+        const float base = m == -INFINITY ? 0.f : m;
+        l = 0.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float by = exp2f(st.m[i][h] - base);   // 0 for a warp that has seen no key
-                l = fmaf(by, st.l[i][h], l);
+        for (int c = 0; c < kCols; ++c) out[c] = 0.f;
 #pragma unroll
-                for (int c = 0; c < kCols; ++c) out[c] = fmaf(by, st.o[i][h][c0 + c], out[c]);
-            }
-            if (whole) {
-                const float inv = 1.f / l;
-                __nv_bfloat16* orow = a.o + ((size_t)s * a.hq + hbase + h) * D + c0;
+        for (int i = 0; i < 4; ++i) {
+            const float by = exp2f(st.m[i][h] - base);       // 0 for a warp that has seen no key
+            l = fmaf(by, st.l[i][h], l);
 #pragma unroll
-                for (int c = 0; c < kCols; ++c) orow[c] = __float2bfloat16_rn(out[c] * inv);
-                if (c0 == 0) a.lse[(size_t)(hbase + h) * a.batch + s] = (m + log2f(l)) * 0.6931471805599453f;
-            } else {
+            for (int c = 0; c < kCols; ++c) out[c] = fmaf(by, st.o[i][h][c0 + c], out[c]);
+        }
+    };
+    auto write = [&](float m, float l, const float (&out)[kCols]) {
+        if (h >= a.group) return;                            // G = 1: the second head does not exist
+        const float inv = 1.f / l;
+        __nv_bfloat16* orow = a.o + ((size_t)s * a.hq + hbase + h) * D + c0;
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) orow[c] = __float2bfloat16_rn(out[c] * inv);
+        if (c0 == 0) a.lse[(size_t)(hbase + h) * a.batch + s] = (m + log2f(l)) * 0.6931471805599453f;
+    };
+    float m, l, out[kCols];
+    if constexpr (kMode == kWhole) {
+        part(0, x1, x1, m, l, out);
+        write(m, l, out);
+    } else if constexpr (kMode == kRuns) {
+        for (int x = x0; x < x1;) {
+            while (bases[s + 1] <= x) ++s;                   // (empty lists)
+            const int first = bases[s], last = bases[s + 1], end = min(x1, last);
+            part(x - first, end - first, last - first, m, l, out);
+            if (x == first && end == last) {
+                write(m, l, out);
+            } else if (h < a.group) {
                 // a run cuts at most two lists: the one it begins in and the one it ends in
-                const size_t slot = (((size_t)kvh * a.runs + blockIdx.y) * 2 + (head ? 1 : 0)) * a.group + h;
+                const size_t slot = (((size_t)kvh * a.runs + blockIdx.y) * 2 + (x == first ? 1 : 0)) * a.group + h;
 #pragma unroll
                 for (int c = 0; c < kCols; ++c) a.part_o[slot * D + c0 + c] = out[c];
                 if (c0 == 0) a.part_ml[slot] = make_float2(m, l);
             }
+            x = end;
+            consumers_sync();                                // (the states are written again)
         }
-        consumers_sync();                                    // (the states are written again)
+    } else {
+        if (x0 < x1) {
+            part(x0, x1, count, m, l, out);
+        } else {                                             // zeros, under a weight of zero
+            m = -INFINITY;
+            l = 0.f;
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) out[c] = 0.f;
+        }
+        // ---- the parts of a list are added up in list order: every CTA of the cluster its share of the columns, 32 to a warp, and every
+        //      warp the maxima and sums of its head, a part to a lane
+        __syncwarp();
+        cluster_wait();                                      // the other CTAs of the cluster have started
+        {
+            const int v = h * D + c0, rank = v / a.share;
+            st_cluster(map_cluster(gather_at + (blockIdx.z * a.share + v - rank * a.share) * 4, rank), out);
+        }
+        if (tid % kPerHead < a.nctas) {
+            const float ml[2] = {m, l};
+            st_cluster(map_cluster(sums_at + (blockIdx.z * kHeads + h) * 8, tid % kPerHead), ml);
+        }
+        __syncwarp();
+        cluster_arrive();
+        cluster_wait();                                      // everything for this CTA is in its shared memory
+        const int v0 = blockIdx.z * a.share, v_end = count > 0 ? min(v0 + a.share, kHeads * D) : 0;
+        for (int v = v0 + tid; v < v_end; v += kD8Consumers) {
+            const int hv = v / D, col = v % D;               // (v - lane is a multiple of 32: the same head in a warp)
+            const float2* sums = reinterpret_cast<const float2*>(behind) + hv;                                       // [CTA][kHeads]
+            const float* parts = reinterpret_cast<const float*>(behind + (gather_at - sums_at)) + (v - v0);           // [CTA][share]
+            const float2 ml = lane < a.nctas ? sums[lane * kHeads] : make_float2(-INFINITY, 0.f);
+            float top = ml.x;
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+            const float w = exp2f(ml.x - (top == -INFINITY ? 0.f : top));     // 0 for a part without entries
+            float sum = w * ml.y;
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+            float o = 0.f;
+#pragma unroll
+            for (int i0 = 0; i0 < kD8MaxCtas; i0 += 4) {     // four at a time, asked for together
+                if (i0 >= a.nctas) break;
+                float wi[4], p[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    wi[i] = __shfl_sync(0xffffffffu, w, i0 + i);
+                    p[i] = parts[min(i0 + i, a.nctas - 1) * a.share];
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i0 + i < a.nctas) o = fmaf(wi[i], p[i], o);
+            }
+            if (hv < a.group) {
+                a.o[((size_t)s * a.hq + hbase + hv) * D + col] = __float2bfloat16_rn(o * (1.f / sum));
+                if (col == 0) a.lse[(size_t)(hbase + hv) * a.batch + s] = (top + log2f(sum)) * 0.6931471805599453f;
+            }
+        }
     }
 }
 
-// Adds up the lists that cuts go through: a CTA per list and KV head.  Parts stand in list order, run by run.
+// Adds up the lists that cuts go through: a CTA per list and KV head, parts in list order, run by run.  The parts' weights first, a
+// thread to each, so that their (max, sum) are asked for at once, as the sums are after that (one after the other was 20 us for 55 parts).
 constexpr int kJoinThreads = 256;
 template <int D>
 __global__ void __launch_bounds__(kJoinThreads) decode8_join_kernel(const Decode8Args a) {
     constexpr int kVec = D / 4;                              // threads to a head's row, 4 columns each
     __shared__ float4 sums[kJoinThreads];
+    __shared__ float weights[kD8MaxRuns * 4];                // [part][head]
+    __shared__ float tops[kJoinThreads / 32][4], ls[kJoinThreads / 32][4];
     pdl_wait();
-    const int kvh = blockIdx.x, s = blockIdx.y, tid = threadIdx.x;
+    const int kvh = blockIdx.x, s = blockIdx.y, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const long long total = a.bases[a.batch], first = a.bases[s], last = a.bases[s + 1];
     if (first == last) return;
     const long long runs = min((long long)a.runs, total);
     auto run_of = [&](long long x) { return (int)(((x + 1) * runs - 1) / total); };   // the last run that begins at or in front of page x
-    const int j0 = run_of(first), j1 = run_of(last - 1);
-    if (j0 == j1) return;                                    // whole: written already
+    const int j0 = run_of(first), j1 = run_of(last - 1), parts = j1 - j0 + 1;
+    if (parts == 1) return;                                  // whole: written already
+    auto slot = [&](int j) { return (((size_t)kvh * a.runs + j) * 2 + (j == j0 ? 1 : 0)) * a.group; };
+    // (tid % group is the same head in every round: 256 is a multiple of the group)
+    const int gh = tid % a.group;
+    float top = -INFINITY;
+    for (int i = tid; i < parts * a.group; i += kJoinThreads) top = fmaxf(top, a.part_ml[slot(j0 + i / a.group) + gh].x);
+#pragma unroll
+    for (int off = 16; off >= 4; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+    for (int off = 2; off >= a.group; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+    if (lane < a.group) tops[warp][lane] = top;
+    __syncthreads();
+    top = tops[0][gh];
+#pragma unroll
+    for (int i = 1; i < kJoinThreads / 32; ++i) top = fmaxf(top, tops[i][gh]);
+    const float base = top == -INFINITY ? 0.f : top;
+    float l = 0.f;
+    for (int i = tid; i < parts * a.group; i += kJoinThreads) {
+        const float2 ml = a.part_ml[slot(j0 + i / a.group) + gh];
+        const float by = exp2f(ml.x - base);
+        weights[i] = by;
+        l = fmaf(by, ml.y, l);
+    }
+#pragma unroll
+    for (int off = 16; off >= 4; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
+    for (int off = 2; off >= a.group; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
+    if (lane < a.group) ls[warp][lane] = l;
+    __syncthreads();
     const int columns = a.group * kVec, groups = kJoinThreads / columns;
     const int g = tid / columns, h = tid % columns / kVec, c = tid % kVec;
-    auto slot = [&](int j) { return (((size_t)kvh * a.runs + j) * 2 + (j == j0 ? 1 : 0)) * a.group + h; };
-    float m = -INFINITY;
-    for (int j = j0; j <= j1; ++j) m = fmaxf(m, a.part_ml[slot(j)].x);
-    const float base = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int j = j0; j <= j1; ++j) {
-        const float2 ml = a.part_ml[slot(j)];
-        const float by = exp2f(ml.x - base);
-        l = fmaf(by, ml.y, l);
-        if ((j - j0) % groups == g) {
-            const float4 v = *reinterpret_cast<const float4*>(a.part_o + slot(j) * D + 4 * c);
-            o.x = fmaf(by, v.x, o.x), o.y = fmaf(by, v.y, o.y), o.z = fmaf(by, v.z, o.z), o.w = fmaf(by, v.w, o.w);
-        }
+    constexpr int kAhead = 8;
+    for (int i0 = g; i0 < parts; i0 += kAhead * groups) {
+        float4 v[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (i0 + u * groups < parts) v[u] = *reinterpret_cast<const float4*>(a.part_o + (slot(j0 + i0 + u * groups) + h) * D + 4 * c);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (i0 + u * groups < parts) {
+                const float by = weights[(i0 + u * groups) * a.group + h];
+                o.x = fmaf(by, v[u].x, o.x), o.y = fmaf(by, v[u].y, o.y), o.z = fmaf(by, v[u].z, o.z), o.w = fmaf(by, v[u].w, o.w);
+            }
     }
     sums[tid] = o;
     __syncthreads();
@@ -458,6 +591,10 @@ __global__ void __launch_bounds__(kJoinThreads) decode8_join_kernel(const Decode
         const float4 v = sums[i * columns + tid];
         o.x += v.x, o.y += v.y, o.z += v.z, o.w += v.w;
     }
+    float m = tops[0][h];
+    l = ls[0][h];
+#pragma unroll
+    for (int i = 1; i < kJoinThreads / 32; ++i) m = fmaxf(m, tops[i][h]), l += ls[i][h];
     const float inv = 1.f / l;
     *reinterpret_cast<uint2*>(a.o + ((size_t)s * a.hq + kvh * a.group + h) * D + 4 * c) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
     if (c == 0) a.lse[(size_t)(kvh * a.group + h) * a.batch + s] = (m + log2f(l)) * 0.6931471805599453f;
@@ -466,6 +603,36 @@ __global__ void __launch_bounds__(kJoinThreads) decode8_join_kernel(const Decode
 int make_page_map(CUtensorMap* m, const void* ptr, int64_t pages, int hkv, int d);   // bf1_attn.cu
 
 typedef void (*Decode8Kernel)(CUtensorMap, CUtensorMap, Decode8Args);
+struct Decode8Variant {
+    Decode8Kernel by_mode[3];            // kRuns, kWhole, kParts
+};
+template <int D, int kHeads>
+static Decode8Variant decode8_variant() {
+    return {{decode8_kernel<D, kHeads, kRuns>, decode8_kernel<D, kHeads, kWhole>, decode8_kernel<D, kHeads, kParts>}};
+}
+
+// Clusters of `ctas` CTAs of a kernel that the GPU runs at once; asked for once per device and shape.
+static int clusters8_that_fit(Decode8Kernel kernel, int dev, int which, int ctas, int stages, size_t smem, int* fit) {
+    static std::atomic<int> known[64][4][kD8MaxCtas + 1][kD8MaxStages + 1];   // 0: not asked yet, else one more
+    std::atomic<int>& k = known[dev][which][ctas][stages];
+    int n = k.load(std::memory_order_relaxed) - 1;
+    if (n < 0) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(1, 1, ctas);
+        cfg.blockDim = dim3(kD8Threads);
+        cfg.dynamicSmemBytes = smem;
+        cudaLaunchAttribute attr = {};
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = attr.val.clusterDim.y = 1;
+        attr.val.clusterDim.z = ctas;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        BF1_CUDA_CHECK(cudaOccupancyMaxActiveClusters(&n, kernel, &cfg));
+        k.store(n + 1, std::memory_order_relaxed);
+    }
+    *fit = n;
+    return BF1_OK;
+}
 static size_t up16(size_t x) { return (x + 15) / 16 * 16; }
 
 }  // namespace bf1
@@ -517,27 +684,61 @@ extern "C" int bf1_decode_fwd_fp8(const void* q, const void* k_pages, const void
     int dev = 0;
     BF1_CUDA_CHECK(cudaGetDevice(&dev));
     if (dev < 0 || dev >= 64) return fail(BF1_ERR_NO_DEVICE, "device ordinal %d out of range", dev);
-    static const Decode8Kernel kernels[4] = {decode8_kernel<64, 2>, decode8_kernel<128, 2>, decode8_kernel<64, 4>, decode8_kernel<128, 4>};
-    const int which = (group == 4 ? 2 : 0) + (d == 128);
-    constexpr int kMostSmem = 100 * 1024;
+    static const Decode8Variant variants[4] = {decode8_variant<64, 2>(), decode8_variant<128, 2>(), decode8_variant<64, 4>(), decode8_variant<128, 4>()};
+    const int heads = group == 4 ? 4 : 2, which = (group == 4 ? 2 : 0) + (d == 128), page_bytes = 2 * kP8 * d;
+    const Decode8Variant& variant = variants[which];
+    constexpr int kMostSmem = 144 * 1024;
     static std::atomic<int> sm_count[64];      // 0: this device has not been set up
     int sms = sm_count[dev].load(std::memory_order_acquire);
     if (!sms) {
-        for (Decode8Kernel k : kernels) BF1_CUDA_CHECK(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem));
+        for (const Decode8Variant& v : variants)
+            for (Decode8Kernel k : v.by_mode) {
+                BF1_CUDA_CHECK(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem));
+                if (k == v.by_mode[kParts]) BF1_CUDA_CHECK(cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+            }
         BF1_CUDA_CHECK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
         sm_count[dev].store(sms, std::memory_order_release);
     }
-    a.runs = batch > kD8MaxScan ? 0 : std::max(1, std::min(3 * sms, kD8MaxRuns) / hkv);
-    a.stages = d == 128 ? 3 : 6;
+    const int64_t lists = (int64_t)batch * hkv;
+    const int most = plan->max_degree;
+    auto ceil_div = [](int64_t x, int64_t y) { return (int)((x + y - 1) / y); };
+    int mode = kRuns;
+    if (batch > kD8MaxScan || (lists >= sms && most <= kD8Held)) mode = kWhole;
+    else if (most <= kD8Held) mode = kParts;
+    a.runs = a.nctas = a.share = 0;
+    size_t smem = 1024;
+    if (mode == kRuns) {
+        a.runs = std::max(1, std::min(3 * sms, kD8MaxRuns) / hkv);
+        a.stages = d == 128 ? 3 : 6;
+        smem += sizeof(int) * (batch + 1);
+    } else if (mode == kWhole) {
+        a.stages = std::min({most, d == 128 ? 6 : 8, kD8MaxStages});
+        if (lists > 2 * sms) a.stages = std::min(a.stages, d == 128 ? 3 : 6);
+    } else {
+        // as many CTAs to a list as still let all clusters run at once (a cluster's CTAs share a GPC, so this is less than what the SMs hold)
+        for (int ctas = (int)std::min<int64_t>({kD8MaxCtas, most, (3 * (int64_t)sms + lists - 1) / lists}); ctas >= 1; --ctas) {
+            const int pages = ceil_div(most, ctas);      // of a CTA, at most
+            ctas = ceil_div(most, pages);                // (no more than that takes)
+            a.nctas = ctas;
+            a.share = ceil_div(heads * d / 32, ctas) * 32;
+            a.stages = std::min(pages, d == 128 ? 4 : 8);
+            smem = 1024 + up16((size_t)ctas * heads * 8) + (size_t)ctas * a.share * 4;
+            if (ctas == 1) break;
+            int fit = 0;
+            if (int rc = clusters8_that_fit(variant.by_mode[kParts], dev, which, ctas, a.stages, smem + (size_t)a.stages * page_bytes, &fit)) return rc;
+            if (lists <= fit) break;
+        }
+    }
+    smem += (size_t)a.stages * page_bytes;
     a.bases = (int32_t*)workspace;
     a.part_ml = (float2*)((uint8_t*)workspace + up16(sizeof(int32_t) * ((size_t)batch + 1)));
     a.part_o = (float*)(a.part_ml + (size_t)hkv * a.runs * 2 * group);
     CUtensorMap tk, tv;
     if (int rc = make_page_map(&tk, k_pages, num_pages, hkv, d)) return rc;
     if (int rc = make_page_map(&tv, v_pages, num_pages, hkv, d)) return rc;
-    const size_t smem = 1024 + (size_t)a.stages * 2 * kP8 * d + sizeof(int) * ((a.runs ? batch : 1) + 1);
-    BF1_CUDA_CHECK(launch_pdl(kernels[which], dim3(hkv, a.runs ? a.runs : batch), kD8Threads, smem, (cudaStream_t)stream, tk, tv, a));
-    if (a.runs)
+    const dim3 grid(hkv, mode == kRuns ? a.runs : batch, mode == kParts ? a.nctas : 1);
+    BF1_CUDA_CHECK(launch_pdl_cluster(variant.by_mode[mode], grid, dim3(1, 1, grid.z), kD8Threads, smem, (cudaStream_t)stream, tk, tv, a));
+    if (mode == kRuns)
         BF1_CUDA_CHECK(launch_pdl(d == 128 ? decode8_join_kernel<128> : decode8_join_kernel<64>, dim3(hkv, batch), kJoinThreads, 0,
                                   (cudaStream_t)stream, a));
     return BF1_OK;
