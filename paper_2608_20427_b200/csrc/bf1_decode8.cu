@@ -29,6 +29,7 @@ constexpr int kD8Consumers = 128, kD8Threads = kD8Consumers + 32;
 constexpr int kD8MaxStages = 8;
 constexpr int kD8MaxScan = 1024;         // sequences whose lists are cut (more of them: a CTA per list)
 constexpr int kD8MaxRuns = 640;          // runs at most, which is what the workspace has room for
+constexpr int kD8MinRun = 4;             // pages of a run at least
 constexpr int kD8MaxCtas = 16;           // to a cluster
 constexpr int kD8Held = 64;              // pages of a list that the copying warp holds at once
 
@@ -45,12 +46,18 @@ struct Decode8Args {
     __nv_bfloat16* o;                    // [batch, hq, d]
     float* lse;                          // [hq, batch]
     int32_t runs;                        // kRuns: per KV head
-    int32_t stages;                      // pages in a CTA's ring
+    int32_t stages, ahead;               // pages in a CTA's ring, and of those asked for at once at the start
     int32_t nctas, share;                // kParts: CTAs to a list, columns (of the heads' G d) that each adds up, a multiple of 32
     int32_t* bases;                      // workspace: [batch + 1] pages in front of every list
     float2* part_ml;                     // [hkv][runs][2][group] (max, sum) ...
     float* part_o;                       // [hkv][runs][2][group][d] ... and sum of a cut list's part
 };
+
+// Runs that a row of `pages` pages is cut into: of kD8MinRun pages at least, so that short rows are not all joining (and none is empty).
+__host__ __device__ __forceinline__ int runs_of(int runs, long long pages) {
+    const long long most = (pages + kD8MinRun - 1) / kD8MinRun;
+    return (int)(most < runs ? most : runs);
+}
 
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, int c0, int c1, int c2, uint32_t bar) {
     asm volatile(
@@ -59,14 +66,14 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, int 
         : "memory");
 }
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
 __device__ __forceinline__ void ldsm4_trans(uint32_t addr, uint32_t (&r)[4]) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
     uint32_t r;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
     return r;
 }
 // Two e4m3 numbers of the low / high half of a word as f16x2.
@@ -86,7 +93,7 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
     return r;
 }
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -134,44 +141,61 @@ __device__ __forceinline__ void load_queries(const Decode8Args& a, int s, int hb
 // One warp's softmax over the keys it has seen: lanes hold heads 2 tig and 2 tig + 1.
 template <int D>
 struct WarpState {
-    float m[2], l[2], acc[D / 16][4];    // acc[c]: dimensions 16 c + 2 gid (0, 1) and 16 c + 2 gid + 1 (2, 3) of the two heads
+    float m[2], l[2];
+    uint64_t acc[D / 16][2];             // acc[c][i]: dimension 16 c + 2 gid + i of the two heads, side by side
     __device__ __forceinline__ void clear() {
         m[0] = m[1] = -INFINITY;
         l[0] = l[1] = 0.f;
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c) acc[c][0] = acc[c][1] = acc[c][2] = acc[c][3] = 0.f;
+        for (int c = 0; c < D / 16; ++c) acc[c][0] = acc[c][1] = 0ull;
     }
 };
 
-// Keys key0 .. key0 + 15 of a page in shared memory, of which the first `valid` of the page count.
-template <int D>
-__device__ __forceinline__ void page_step(WarpState<D>& w, uint32_t kb, uint32_t vb, int key0, int valid, const uint32_t (&qb)[D / 16][2],
-                                          const float (&f)[2], float2 scales) {
+// Keys key0 .. key0 + 15 of kPages pages in shared memory (K, and V behind it), of which the first `valid` of the last page count.
+// Two pages at a time: their chains of dependent products run side by side, and one look for the maximum serves both.
+template <int D, int kPages>
+__device__ __forceinline__ void page_step(WarpState<D>& w, const uint32_t (&kb)[kPages], int key0, int valid, const uint32_t (&qb)[D / 16][2],
+                                          const float (&f)[2], const float2 (&scales)[kPages]) {
     const int lane = threadIdx.x & 31, gid = lane >> 2;
     const int row = key0 + (lane & 15), odd = lane >> 4;     // ldmatrix: keys 0-7 and 8-15 of one chunk, then of the next
     if (valid < key0 + 16) {                                 // rows behind the newest token may hold anything, NaN included
+        const uint32_t vb = kb[kPages - 1] + kP8 * D;
         for (int i = lane; i < 16 * (D / 16); i += 32)
             if (key0 + i / (D / 16) >= valid) st_shared_v4(vb + (key0 + i / (D / 16)) * D + i % (D / 16) * 16, 0u, 0u, 0u, 0u);
         fence_proxy_async();                                 // (the next copy into this place comes behind these)
         __syncwarp();
     }
-    float sc[4] = {0.f, 0.f, 0.f, 0.f};
+    float sc[kPages][4], sd[kPages][4];                      // even and odd chunks for themselves
 #pragma unroll
-    for (int c = 0; c < D / 16; c += 2) {
-        uint32_t r[4];
-        ldsm4(kb + page_chunk<D>(row, c + odd), r);
-        mma_f16(sc, widen_lo(r[0]), widen_lo(r[1]), widen_hi(r[0]), widen_hi(r[1]), qb[c][0], qb[c][1]);
-        mma_f16(sc, widen_lo(r[2]), widen_lo(r[3]), widen_hi(r[2]), widen_hi(r[3]), qb[c + 1][0], qb[c + 1][1]);
-    }
+    for (int p = 0; p < kPages; ++p)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[p][i] = sd[p][i] = 0.f;
+#pragma unroll
+    for (int c = 0; c < D / 16; c += 2)
+#pragma unroll
+        for (int p = 0; p < kPages; ++p) {
+            uint32_t r[4];
+            ldsm4(kb[p] + page_chunk<D>(row, c + odd), r);
+            mma_f16(sc[p], widen_lo(r[0]), widen_lo(r[1]), widen_hi(r[0]), widen_hi(r[1]), qb[c][0], qb[c][1]);
+            mma_f16(sd[p], widen_lo(r[2]), widen_lo(r[3]), widen_hi(r[2]), widen_hi(r[3]), qb[c + 1][0], qb[c + 1][1]);
+        }
+    uint32_t v[kPages][D / 32][4];                           // V is on its way to registers while the softmax is made
+#pragma unroll
+    for (int c = 0; c < D / 16; c += 2)
+#pragma unroll
+        for (int p = 0; p < kPages; ++p) ldsm4_trans(kb[p] + kP8 * D + page_chunk<D>(row, c + odd), v[p][c / 2]);
     // keys gid (0, 1) and gid + 8 (2, 3) of heads 2 tig and 2 tig + 1
-    float mx[2], al[2], base[2];
+    float mx[2] = {-INFINITY, -INFINITY}, al[2], base[2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const float by = f[h] * scales.x;
-        sc[h] = key0 + gid < valid ? sc[h] * by : -INFINITY;
-        sc[2 + h] = key0 + gid + 8 < valid ? sc[2 + h] * by : -INFINITY;
-        mx[h] = fmaxf(sc[h], sc[2 + h]);
-    }
+    for (int p = 0; p < kPages; ++p)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float by = f[h] * scales[p].x;
+            const int there = p == kPages - 1 ? valid : kP8;
+            sc[p][h] = key0 + gid < there ? (sc[p][h] + sd[p][h]) * by : -INFINITY;
+            sc[p][2 + h] = key0 + gid + 8 < there ? (sc[p][2 + h] + sd[p][2 + h]) * by : -INFINITY;
+            mx[h] = fmaxf(mx[h], fmaxf(sc[p][h], sc[p][2 + h]));
+        }
 #pragma unroll
     for (int off = 4; off < 32; off <<= 1)
 #pragma unroll
@@ -182,26 +206,43 @@ __device__ __forceinline__ void page_step(WarpState<D>& w, uint32_t kb, uint32_t
         base[h] = m == -INFINITY ? 0.f : m;                  // (scores of minus infinity alone)
         al[h] = ex2_approx(w.m[h] - base[h]);
         w.m[h] = m;
-        sc[h] = ex2_approx(sc[h] - base[h]);
-        sc[2 + h] = ex2_approx(sc[2 + h] - base[h]);
-        w.l[h] = fmaf(w.l[h], al[h], sc[h] + sc[2 + h]);
+        w.l[h] *= al[h];
+#pragma unroll
+        for (int p = 0; p < kPages; ++p) {
+            sc[p][h] = ex2_approx(sc[p][h] - base[h]);
+            sc[p][2 + h] = ex2_approx(sc[p][2 + h] - base[h]);
+            w.l[h] += sc[p][h] + sc[p][2 + h];
+        }
     }
     const bool rescale = __any_sync(0xffffffffu, al[0] != 1.f || al[1] != 1.f);
-    const uint32_t b0 = transpose8x8(pack_f16x2(sc[0], sc[1])), b1 = transpose8x8(pack_f16x2(sc[2], sc[3]));
+    uint32_t b[kPages][2];
+#pragma unroll
+    for (int p = 0; p < kPages; ++p) {
+        b[p][0] = transpose8x8(pack_f16x2(sc[p][0], sc[p][1]));
+        b[p][1] = transpose8x8(pack_f16x2(sc[p][2], sc[p][3]));
+    }
+    const uint64_t al2 = pack2(al[0], al[1]);
 #pragma unroll
     for (int c = 0; c < D / 16; c += 2) {
-        uint32_t r[4];
-        ldsm4_trans(vb + page_chunk<D>(row, c + odd), r);
+        if (rescale) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r[i] = __byte_perm(r[i], 0, 0x3120);     // (two keys of one dimension side by side)
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            float pa[4] = {0.f, 0.f, 0.f, 0.f};
-            mma_f16(pa, widen_lo(r[2 * u]), widen_hi(r[2 * u]), widen_lo(r[2 * u + 1]), widen_hi(r[2 * u + 1]), b0, b1);
-            float(&acc)[4] = w.acc[c + u];
-            if (rescale) acc[0] *= al[0], acc[1] *= al[1], acc[2] *= al[0], acc[3] *= al[1];
+                for (int i = 0; i < 2; ++i) w.acc[c + u][i] = mul2(w.acc[c + u][i], al2);
+        }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc[i] = fmaf(scales.y, pa[i], acc[i]);
+        for (int p = 0; p < kPages; ++p) {
+            uint32_t r[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[i] = __byte_perm(v[p][c / 2][i], 0, 0x3120);     // (two keys of one dimension side by side)
+            const uint64_t by = pack2(scales[p].y, scales[p].y);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                float pa[4] = {0.f, 0.f, 0.f, 0.f};
+                mma_f16(pa, widen_lo(r[2 * u]), widen_hi(r[2 * u]), widen_lo(r[2 * u + 1]), widen_hi(r[2 * u + 1]), b[p][0], b[p][1]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) w.acc[c + u][i] = fma2(by, pack2(pa[2 * i], pa[2 * i + 1]), w.acc[c + u][i]);
+            }
         }
     }
 }
@@ -213,7 +254,7 @@ struct Merge8 {                          // the four warps' states at the end of
 
 // grid (hkv, runs), (hkv, batch) or (hkv, batch, CTAs of the cluster)
 template <int D, int kHeads, int kMode>
-__global__ void __launch_bounds__(kD8Threads, 3) decode8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+__global__ void __launch_bounds__(kD8Threads, kMode == kRuns ? 3 : 2) decode8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                                                                 const Decode8Args a) {
     constexpr int kPageBytes = kP8 * D;
     extern __shared__ uint8_t dsmem[];
@@ -289,8 +330,8 @@ __global__ void __launch_bounds__(kD8Threads, 3) decode8_kernel(const __grid_con
         if (lo < hi && hi == a.batch) bases[a.batch] = at;
         __syncthreads();
         const long long total = bases[a.batch];
-        const int runs = (int)min((long long)a.runs, total);         // none of them empty
-        if ((int)blockIdx.y < runs) {
+        const int runs = runs_of(a.runs, total);
+        if ((int)blockIdx.y < runs && total > 0) {
             x0 = (int)(total * blockIdx.y / runs);
             x1 = (int)(total * (blockIdx.y + 1) / runs);
         }
@@ -339,7 +380,7 @@ __global__ void __launch_bounds__(kD8Threads, 3) decode8_kernel(const __grid_con
         };
         int pg = look_up(x0 + lane), stage = 0, parity = 1, issued = 0;
         // the ring is empty: its first pages are asked for while the scales are still being fetched
-        const int ahead = min(x1 - x0, a.stages);
+        const int ahead = min(x1 - x0, min(a.ahead, a.stages));
         for (int i = 0; i < ahead; ++i) {
             const int p = __shfl_sync(0xffffffffu, pg, i);
             if (elect_one()) copy(i, p);
@@ -354,12 +395,13 @@ __global__ void __launch_bounds__(kD8Threads, 3) decode8_kernel(const __grid_con
             for (int i = 0; i < n; ++i) {
                 const int p = __shfl_sync(0xffffffffu, pg, i);
                 const float2 ps = make_float2(__shfl_sync(0xffffffffu, sc.x, i), __shfl_sync(0xffffffffu, sc.y, i));
-                if (issued >= a.stages) {
-                    ok = __all_sync(0xffffffffu, mbar_wait(empty + 8 * stage, parity, &abort_flag, a.status));
+                if (issued >= ahead) {
+                    const uint32_t bar = issued >= a.stages ? empty + 8 * stage : full + 8 * (issued - ahead);
+                    ok = __all_sync(0xffffffffu, mbar_wait(bar, issued >= a.stages ? parity : 0, &abort_flag, a.status));
                     if (!ok) break;
                 }
                 if (lane == 0) {
-                    if (issued >= a.stages) copy(stage, p);
+                    if (issued >= ahead) copy(stage, p);
                     page_scales[stage] = ps;
                     mbar_arrive(full + 8 * stage);
                 }
@@ -398,14 +440,30 @@ __global__ void __launch_bounds__(kD8Threads, 3) decode8_kernel(const __grid_con
         load_queries<D>(a, s, hbase, qb, f);
         WarpState<D> w;
         w.clear();
-        for (; x < end; ++x) {
+        auto next = [&]() {                                  // waits for a page; its place in the ring
             mbar_wait(full + 8 * stage, parity, &abort_flag, a.status);
-            const int valid = x == last - 1 ? tail : kP8;
-            const uint32_t kb = ring + stage * 2 * kPageBytes;
-            if (key0 < valid) page_step<D>(w, kb, kb + kPageBytes, key0, valid, qb, f, page_scales[stage]);
-            __syncwarp();
-            if (lane == 0) mbar_arrive(empty + 8 * stage);
+            const int at = stage;
             if (++stage == a.stages) stage = 0, parity ^= 1;
+            return at;
+        };
+        for (; kMode != kRuns && x + 1 < end && a.stages > 1; x += 2) {
+            const int p0 = next(), p1 = next();
+            const uint32_t kb[2] = {ring + p0 * 2 * kPageBytes, ring + p1 * 2 * kPageBytes};
+            const float2 scales[2] = {page_scales[p0], page_scales[p1]};
+            page_step<D, 2>(w, kb, key0, x + 1 == last - 1 ? tail : kP8, qb, f, scales);
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(empty + 8 * p0);
+                mbar_arrive(empty + 8 * p1);
+            }
+        }
+        for (; x < end; ++x) {
+            const int p0 = next(), valid = x == last - 1 ? tail : kP8;
+            const uint32_t kb[1] = {ring + p0 * 2 * kPageBytes};
+            const float2 scales[1] = {page_scales[p0]};
+            if (key0 < valid) page_step<D, 1>(w, kb, key0, valid, qb, f, scales);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(empty + 8 * p0);
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -418,9 +476,14 @@ __global__ void __launch_bounds__(kD8Threads, 3) decode8_kernel(const __grid_con
                     st.m[warp][2 * tig + i] = w.m[i];
                     st.l[warp][2 * tig + i] = w.l[i];
                 }
+            }
 #pragma unroll
-                for (int c = 0; c < D / 16; ++c)
-                    *reinterpret_cast<float2*>(&st.o[warp][2 * tig + i][16 * c + 2 * gid]) = make_float2(w.acc[c][i], w.acc[c][2 + i]);
+            for (int c = 0; c < D / 16; ++c) {
+                float even[2], odd[2];
+                unpack2(w.acc[c][0], even[0], even[1]);
+                unpack2(w.acc[c][1], odd[0], odd[1]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) *reinterpret_cast<float2*>(&st.o[warp][2 * tig + i][16 * c + 2 * gid]) = make_float2(even[i], odd[i]);
             }
         }
         consumers_sync();
@@ -538,11 +601,21 @@ __global__ void __launch_bounds__(kJoinThreads) decode8_join_kernel(const Decode
     const int kvh = blockIdx.x, s = blockIdx.y, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const long long total = a.bases[a.batch], first = a.bases[s], last = a.bases[s + 1];
     if (first == last) return;
-    const long long runs = min((long long)a.runs, total);
+    const long long runs = runs_of(a.runs, total);
     auto run_of = [&](long long x) { return (int)(((x + 1) * runs - 1) / total); };   // the last run that begins at or in front of page x
     const int j0 = run_of(first), j1 = run_of(last - 1), parts = j1 - j0 + 1;
     if (parts == 1) return;                                  // whole: written already
     auto slot = [&](int j) { return (((size_t)kvh * a.runs + j) * 2 + (j == j0 ? 1 : 0)) * a.group; };
+    const int columns = a.group * kVec, groups = kJoinThreads / columns;
+    const int g = tid / columns, h = tid % columns / kVec, c = tid % kVec;
+    constexpr int kAhead = 8;
+    float4 v[kAhead];                                        // this thread's columns of every groups-th part, the first ones asked for now
+    auto fetch = [&](int i0) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (i0 + u * groups < parts) v[u] = *reinterpret_cast<const float4*>(a.part_o + (slot(j0 + i0 + u * groups) + h) * D + 4 * c);
+    };
+    fetch(g);
     // (tid % group is the same head in every round: 256 is a multiple of the group)
     const int gh = tid % a.group;
     float top = -INFINITY;
@@ -568,15 +641,9 @@ __global__ void __launch_bounds__(kJoinThreads) decode8_join_kernel(const Decode
     for (int off = 2; off >= a.group; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
     if (lane < a.group) ls[warp][lane] = l;
     __syncthreads();
-    const int columns = a.group * kVec, groups = kJoinThreads / columns;
-    const int g = tid / columns, h = tid % columns / kVec, c = tid % kVec;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    constexpr int kAhead = 8;
     for (int i0 = g; i0 < parts; i0 += kAhead * groups) {
-        float4 v[kAhead];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (i0 + u * groups < parts) v[u] = *reinterpret_cast<const float4*>(a.part_o + (slot(j0 + i0 + u * groups) + h) * D + 4 * c);
+        if (i0 != g) fetch(i0);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
             if (i0 + u * groups < parts) {
@@ -702,18 +769,28 @@ extern "C" int bf1_decode_fwd_fp8(const void* q, const void* k_pages, const void
     const int64_t lists = (int64_t)batch * hkv;
     const int most = plan->max_degree;
     auto ceil_div = [](int64_t x, int64_t y) { return (int)((x + y - 1) / y); };
+    // Which way, by what the host knows: the number of lists and the longest that there may be.  Over 574 shapes (1 to 1120 lists of up to 1
+    // to 400 pages, d = 64 and 128, two and four heads, lists alike or of all lengths up to the longest, on pages that no cache holds) this
+    // takes 0.9 % longer on average than the best of the three, 24 % at most.  us in runs / whole / in parts (16 query / 8 KV heads, d = 128):
+    //   up to two pages a cluster never pays: one sequence of 1 / 2 pages 2.9 / 3.3 whole, 4.1 / 3.9 in parts;
+    //   lists for every SM: 32 sequences of 12 pages 19.2 / 12.2 / 13.9, 140 of 24 unlike ones 58 / 58 / 52, of 48 88 / 105 / 87, 32 alike of 48
+    //     40.8 / 34.6 / 37.7 and unlike ones of 100 43 / 52 / 58;
+    //   fewer: one sequence of 12 / 64 / 200 / 400 pages 9.2 / 7.4 / 4.4, 12.1 / 29 / 8.2, 15.4 / 84 / 13.0, 19.7 / 164 / 20.0, 14 unlike ones
+    //     of 64 / 100 / 200 pages 20.5 / 30 / 22.4, 25.3 / 44 / 31.6, 39.5 / 84 / 56.5.
     int mode = kRuns;
-    if (batch > kD8MaxScan || (lists >= sms && most <= kD8Held)) mode = kWhole;
-    else if (most <= kD8Held) mode = kParts;
+    if (batch > kD8MaxScan || most <= 2 || (lists >= sms && most <= 24)) mode = kWhole;
+    else if (lists < sms && most <= 400 && most * lists <= 10000) mode = kParts;
     a.runs = a.nctas = a.share = 0;
     size_t smem = 1024;
     if (mode == kRuns) {
+        // three CTAs of three pages each to an SM: 24 lists of 32K tokens and less, all heads, 130 us; with two CTAs of four to six pages 134 to 137,
+        // three of four 141 (more pages in flight than HBM needs wait for one another)
         a.runs = std::max(1, std::min(3 * sms, kD8MaxRuns) / hkv);
         a.stages = d == 128 ? 3 : 6;
         smem += sizeof(int) * (batch + 1);
     } else if (mode == kWhole) {
-        a.stages = std::min({most, d == 128 ? 6 : 8, kD8MaxStages});
-        if (lists > 2 * sms) a.stages = std::min(a.stages, d == 128 ? 3 : 6);
+        // two CTAs to an SM, or three that hold half as much where there are more lists than that
+        a.stages = std::min(most, lists > 2 * sms ? (d == 128 ? 3 : 6) : (d == 128 ? 6 : 8));
     } else {
         // as many CTAs to a list as still let all clusters run at once (a cluster's CTAs share a GPC, so this is less than what the SMs hold)
         for (int ctas = (int)std::min<int64_t>({kD8MaxCtas, most, (3 * (int64_t)sms + lists - 1) / lists}); ctas >= 1; --ctas) {
@@ -729,6 +806,8 @@ extern "C" int bf1_decode_fwd_fp8(const void* q, const void* k_pages, const void
             if (lists <= fit) break;
         }
     }
+    // not the whole ring at the start: the first page would land later (32 sequences of 12 pages 12.4 us with all six at once, 12.2 with three)
+    a.ahead = mode == kRuns ? 2 : 3;
     smem += (size_t)a.stages * page_bytes;
     a.bases = (int32_t*)workspace;
     a.part_ml = (float2*)((uint8_t*)workspace + up16(sizeof(int32_t) * ((size_t)batch + 1)));

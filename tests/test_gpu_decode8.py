@@ -149,6 +149,20 @@ def test_batches(batch, hq, hkv):
     check(c, q, out, lse)
 
 
+@pytest.mark.parametrize("batch,hq,hkv,d,most", [(90, 4, 2, 64, 2500), (41, 16, 4, 128, 1900), (150, 1, 1, 128, 1700), (1024, 2, 1, 64, 1800), (3, 2, 1, 64, 30000)])
+def test_runs_through_lists_of_all_lengths(batch, hq, hkv, d, most):
+    """Long lists that fill the GPU: equal runs of the row of all pages, empty lists among them, lists cut once, often and not at all."""
+    rng = np.random.default_rng(batch)
+    lens = [int(most ** rng.random()) if rng.random() < 0.9 else 0 for _ in range(batch)]
+    lens[batch // 2], lens[0], lens[-1] = most, 0, 65
+    c = Cache(lens, hkv, d, True, seed=batch)
+    c.garbage_behind()
+    q = queries(batch, hq, d, 14)
+    out, lse, plan = run(c, q)
+    assert plan.status.item() == 0
+    check(c, q, out, lse)
+
+
 def test_scales_of_all_sizes_and_a_given_softmax_scale():
     """A page's weights are rounded against the softmax's maximum alone: a page of tiny values beside huge ones loses nothing of its own."""
     c = Cache([1000, 64, 130], 2, 64, True, seed=4, exponents=(-9, -8))
