@@ -10,6 +10,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
 #include <c10/cuda/CUDAGuard.h>
@@ -100,6 +101,17 @@ struct Place {
         }
     }
 };
+// A new tensor on the current device's current stream, without a way through the dispatcher.
+at::Tensor fresh(at::IntArrayRef sizes, const at::Tensor& like, at::ScalarType type) {
+    return at::detail::empty_cuda(sizes, type, like.device(), std::nullopt);
+}
+// A part of `flat`'s memory as a contiguous tensor of its own.
+at::Tensor part_of(const at::Tensor& flat, int64_t offset, at::IntArrayRef sizes) {
+    at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(flat.storage()), flat.key_set(), flat.dtype());
+    t.unsafeGetTensorImpl()->set_storage_offset(offset);
+    t.unsafeGetTensorImpl()->set_sizes_contiguous(sizes);
+    return t;
+}
 // [tokens, heads, d] bf16 with the dimensions of a head side by side, on `like`'s device
 bf1_rows rows_of(const at::Tensor& t, const at::Tensor& like, const char* what) {
     require(t.device() == like.device() && t.scalar_type() == at::kBFloat16 && t.dim() == 3 && (t.size(2) == 1 || t.stride(2) == 1), what);
@@ -280,8 +292,15 @@ PyObject* rope(PyObject* const* a) {
     require(k.size(0) == q.size(0) && k.size(2) == q.size(2), "q and k must have the same tokens and head dimension");
     const auto* pp = array_of<const int32_t>(pos, q, at::kInt, "positions must be a contiguous int32 tensor on the same device");
     require(pos.dim() == 1 && pos.size(0) == q.size(0), "positions must have an entry for every token");
-    const at::Tensor out_q = a[6] == Py_None ? at::empty(q.sizes(), q.options()) : tensor(a[6]);
-    const at::Tensor out_k = !keys ? out_q : a[7] == Py_None ? at::empty(k.sizes(), k.options()) : tensor(a[7]);
+    at::Tensor out_q, out_k;
+    if (keys && a[6] == Py_None && a[7] == Py_None) {    // both in one piece of memory: a second allocation would cost as much as the kernel's launch
+        const at::Tensor flat = fresh({q.numel() + k.numel()}, q, at::kBFloat16);
+        out_q = part_of(flat, 0, q.sizes());
+        out_k = part_of(flat, q.numel(), k.sizes());
+    } else {
+        out_q = a[6] == Py_None ? fresh(q.sizes(), q, at::kBFloat16) : tensor(a[6]);
+        out_k = !keys ? out_q : a[7] == Py_None ? fresh(k.sizes(), q, at::kBFloat16) : tensor(a[7]);
+    }
     require(out_q.sizes() == q.sizes() && out_k.sizes() == (keys ? k : q).sizes(), "the outputs must have the shapes of q and k");
     const bf1_rows oq = rows_of(out_q, q, what), ok = rows_of(out_k, q, what);
     const int32_t tokens = q.size(0), hq = q.size(1), hkv = keys ? k.size(1) : 0, d = q.size(2);

@@ -2,8 +2,8 @@
 //
 // A pair of dimensions (x, y) of a head at position p becomes (x cos a - y sin a, x sin a + y cos a) with a = p * f_i, the pair's
 // frequency.  Every value is read once and written once, 4 bytes in all: bound by HBM for long batches, by one chain of launch,
-// position, table and row for short ones.  The angles would be the arithmetic to pay for (64-bit product, sine and cosine); a thread makes
-// the eight of its pairs once and turns the same pairs of every head with them.
+// position, table and row for short ones.  The angles would be the arithmetic to pay for (64-bit product, sine and cosine); they are
+// made once for a token and turn the same pairs of every head.
 #include <math.h>
 
 #include <algorithm>
@@ -12,27 +12,23 @@
 
 namespace bf1 {
 
-constexpr int kRopeThreads = 128;
-constexpr int kRopeAhead = 4;      // heads asked for before the first of them is turned: 8 loads of 16 bytes a thread
-
+// Heads asked for before the first of them is turned: more CTAs on an SM count for more than more loads of each.  1 / 2 / 3 / 4 / 6: 4096
+// tokens of 24 heads, forward and gradient, 22.7 / 19.8 / 23.1 / 23.5 / 23.0 us, 32768 forward 65.3 / 64.1 / 67.5 / 67.2 / 66.0.
+constexpr int kRopeAhead = 2;
 struct RopeArgs {
     Rows q, k, out_q, out_k;
     const int32_t* positions;
     RopeTable rope;
     int32_t tokens, hq, heads;     // heads: of q and k together
-    int32_t per_token;             // threads of a token: d / 16
     float sign;
 };
 
-// blockIdx.x: tokens, per_token threads to each; blockIdx.y: of gridDim.y shares of the heads.
+// blockIdx.x: tokens; blockIdx.y: one of gridDim.y shares of the heads
+template <int D>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs a) {
     pdl_wait();
-    const int64_t token = (int64_t)blockIdx.x * (kRopeThreads / a.per_token) + threadIdx.x / a.per_token;
-    if (token >= a.tokens) return;
-    const int position = a.positions[token];
-    if (position < 0) return;                            // padding: its rows stay as they are
-    rope_heads<kRopeAhead>(a.rope, position, token, threadIdx.x % a.per_token, a.sign, a.q, a.k, a.out_q, a.out_k, a.hq, a.heads,
-                           blockIdx.y, gridDim.y);
+    rope_block<D, kRopeAhead>(a.rope, a.positions, (int64_t)blockIdx.x * kRopeTokens<D>, a.tokens, a.sign, a.q, a.k, a.out_q, a.out_k, a.hq, a.heads,
+                              4 * blockIdx.y, 4 * gridDim.y);
 }
 
 int check_rows(const bf1_rows* rows, const char* name) {
@@ -76,11 +72,11 @@ static int rope_call(const bf1_rows* q, const bf1_rows* k, const int32_t* positi
     a.tokens = tokens;
     a.hq = hq;
     a.heads = hq + hkv;
-    a.per_token = d / 16;
     a.sign = sign;
-    const int per_cta = kRopeThreads / a.per_token, ctas = (tokens + per_cta - 1) / per_cta;
-    const int shares = std::max(1, std::min(a.heads, 148 * 8 / ctas));
-    BF1_CUDA_CHECK(launch_pdl(rope_kernel, dim3(ctas, shares), kRopeThreads, 0, (cudaStream_t)stream, a));
+    // few tokens: their heads are shared out, four at least to a CTA
+    const int ctas = d == 128 ? (tokens + kRopeTokens<128> - 1) / kRopeTokens<128> : (tokens + kRopeTokens<64> - 1) / kRopeTokens<64>;
+    const int shares = std::max(1, std::min((a.heads + 3) / 4, 148 * 8 / ctas));
+    BF1_CUDA_CHECK(launch_pdl(d == 128 ? rope_kernel<128> : rope_kernel<64>, dim3(ctas, shares), kRopeThreads, 0, (cudaStream_t)stream, a));
     return BF1_OK;
 }
 
