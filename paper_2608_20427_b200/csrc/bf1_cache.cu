@@ -14,6 +14,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cfloat>
+#include <type_traits>
 
 #include "bf1_rope.cuh"
 
@@ -435,11 +436,19 @@ __global__ void __launch_bounds__(128) cache_write_pages_kernel(const WriteArgs 
     }
     if constexpr (kRope) {
         float x[kPer][8], top = 0.f;
+        __shared__ float2 angles[kRows][D / 2];
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
+            if (i * kRows >= u.y) break;
+            __syncthreads();                             // the rows of the round before have been turned
+            for (int j = threadIdx.x; j < kRows * D / 2; j += 128) {
+                const int r = i * kRows + j / (D / 2), pair = j % (D / 2);
+                if (r < u.y && 2 * pair < a.rope.dim) angles[j / (D / 2)][pair] = rope_angle(a.rope, a.positions[u.x + r], pair);
+            }
+            __syncthreads();
             const int r = r0 + i * kRows;
             if (r < u.y) {
-                rope_chunk(a.rope, a.positions[u.x + r], in.at((int64_t)u.x + r, h), c, x[i]);
+                rope_chunk(a.rope, in.at((int64_t)u.x + r, h), c, x[i], [&](int pair) { return angles[r0][pair]; });
                 top = magnitude_of(x[i], top);
             }
         }
@@ -484,37 +493,64 @@ __global__ void __launch_bounds__(128) cache_write_tokens_kernel(const WriteArgs
         return;
     }
     const Rows& in = a.x[which];
+    // the angles of kRows rows, D / 2 pairs to each: two to a lane, in 64 bits where numbers in 8 bits come of them
+    using Angle = typename std::conditional<kFp8, double2, float2>::type;
+    __shared__ Angle angles[kRope ? 4 : 1][kRope ? 64 : 1];
+    auto turn_rows = [&](int rb) {
+        if constexpr (kRope) {
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int i = lane + 32 * j, r = rb + i / (D / 2), pair = i % (D / 2);
+                if (r < u.y && 2 * pair < a.rope.dim) {
+                    if constexpr (kFp8) angles[threadIdx.x >> 5][i] = rope_angle64(a.rope, a.positions[u.x + r], pair);
+                    else angles[threadIdx.x >> 5][i] = rope_angle(a.rope, a.positions[u.x + r], pair);
+                }
+            }
+            __syncwarp();
+        }
+    };
     auto load = [&](int r, float (&x)[8]) {
         const __nv_bfloat16* row = in.at((int64_t)u.x + r, h);
-        if (kRope && which == 0) rope_chunk(a.rope, a.positions[u.x + r], row, c, x);
-        else unpack_bf16x8(*reinterpret_cast<const uint4*>(row + 8 * c), x);
+        if constexpr (kRope) {
+            if (which == 0) return rope_chunk(a.rope, row, c, x, [&](int pair) { return angles[threadIdx.x >> 5][r0 * (D / 2) + pair]; });
+        }
+        unpack_bf16x8(*reinterpret_cast<const uint4*>(row + 8 * c), x);
     };
     const size_t pitch = (size_t)a.hkv * D;
     const size_t first = ((size_t)u.z * kCachePage) * pitch + (size_t)h * D + 8 * c;
     float x[8];
     if constexpr (!kFp8) {
         __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.pages[which]) + first;
-        for (int r = r0; r < u.y; r += kRows) {
-            load(r, x);
-            *reinterpret_cast<uint4*>(out + (u.w + r) * pitch) = pack_bf16x8(x);
+        for (int rb = 0; rb < u.y; rb += kRows) {
+            turn_rows(rb);
+            if (rb + r0 < u.y) {
+                load(rb + r0, x);
+                *reinterpret_cast<uint4*>(out + (u.w + rb + r0) * pitch) = pack_bf16x8(x);
+            }
         }
         return;
     }
     float* const at = a.scales[which] + (size_t)u.z * a.hkv + h;
     const float before = u.w > 0 ? *at : 0.f;
     float top = 0.f;
-    for (int r = r0 + (u.y - 1) / kRows * kRows; r >= 0; r -= kRows)       // the first rows last: they stay in x
-        if (r < u.y) {
-            load(r, x);
+    for (int rb = (u.y - 1) / kRows * kRows; rb >= 0; rb -= kRows) {       // the first rows last: they stay in x
+        turn_rows(rb);
+        if (rb + r0 < u.y) {
+            load(rb + r0, x);
             top = magnitude_of(x, top);
         }
+    }
 #pragma unroll
     for (int off = 8; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
     const float scale = fmaxf(scale_for(top), before), inv = 1.f / scale;
     uint8_t* out = a.pages[which] + first;
-    for (int r = r0; r < u.y; r += kRows) {
-        if (r != r0) load(r, x);
-        *reinterpret_cast<uint2*>(out + (u.w + r) * pitch) = quantize(x, inv);
+    for (int rb = 0; rb < u.y; rb += kRows) {
+        if (rb > 0) turn_rows(rb);
+        if (rb + r0 < u.y) {
+            if (rb > 0) load(rb + r0, x);
+            *reinterpret_cast<uint2*>(out + (u.w + rb + r0) * pitch) = quantize(x, inv);
+        }
     }
     if (u.w > 0 && before != scale) {
         constexpr int kAhead = 8;

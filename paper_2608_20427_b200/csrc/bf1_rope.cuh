@@ -16,13 +16,24 @@ struct RopeTable {
 
 // (cos, sin) of a pair's angle, times the magnitude.  The angle is position * turns in 64 bits, of which only the part of a turn
 // counts: exact to 2^-53 of the whole, so that a position of 2^31 still has 1e-7 of a radian, where 32 bits lose all of it
-// beyond 2^24 turns.
+// beyond 2^24 turns.  In 32 bits the sine and cosine are those of the rounded angle, corrected by their slopes times what the rounding
+// took (which would be as large as their own error).  In 64 bits a call costs 2.5 times as much: it is for numbers that are rounded
+// to three bits of fraction next, where an error of 2^-24 may turn a tie.
+__device__ __forceinline__ double rope_half_turns(const RopeTable& r, int position, int pair) {
+    const double t = (double)position * r.turns[pair];
+    return 2.0 * (t - rint(t));
+}
 __device__ __forceinline__ float2 rope_angle(const RopeTable& r, int position, int pair) {
-    double t = (double)position * r.turns[pair];
-    t -= rint(t);
+    const double t = rope_half_turns(r, position, pair);
+    const float hi = (float)t, lo = 3.14159265f * (float)(t - (double)hi);
     float s, c;
-    sincospif(2.f * (float)t, &s, &c);
-    return make_float2(c * r.magnitude, s * r.magnitude);
+    sincospif(hi, &s, &c);
+    return make_float2(__fmaf_rn(-lo, s, c) * r.magnitude, __fmaf_rn(lo, c, s) * r.magnitude);
+}
+__device__ __forceinline__ double2 rope_angle64(const RopeTable& r, int position, int pair) {
+    double s, c;
+    sincospi(rope_half_turns(r, position, pair), &s, &c);
+    return make_double2(c * r.magnitude, s * r.magnitude);
 }
 
 __device__ __forceinline__ void unpack_bf16x8(const uint4& v, float (&x)[8]) {
@@ -42,6 +53,12 @@ __device__ __forceinline__ void rope_turn(float& x, float& y, float c, float s) 
     const float p = x, q = y;
     x = __fmaf_rn(p, c, -__fmul_rn(q, s));
     y = __fmaf_rn(p, s, __fmul_rn(q, c));
+}
+
+__device__ __forceinline__ void rope_turn(float& x, float& y, double c, double s) {
+    const double p = x, q = y;
+    x = (float)(p * c - q * s);
+    y = (float)(p * s + q * c);
 }
 
 // Rows of heads in global memory: bf16, the dimensions of a head side by side, strides in elements.
@@ -121,8 +138,9 @@ __device__ __forceinline__ void rope_block(const RopeTable& r, const int32_t* po
     }
 }
 
-// Dimensions 8 c .. 8 c + 7 of a row, rotated.
-__device__ __forceinline__ void rope_chunk(const RopeTable& r, int position, const __nv_bfloat16* row, int c, float (&x)[8]) {
+// Dimensions 8 c .. 8 c + 7 of a row, rotated by angle(pair) = (cos, sin).
+template <typename F>
+__device__ __forceinline__ void rope_chunk(const RopeTable& r, const __nv_bfloat16* row, int c, float (&x)[8], F&& angle) {
     unpack_bf16x8(*reinterpret_cast<const uint4*>(row + 8 * c), x);
     if (8 * c >= r.dim) return;
     if (r.half) {
@@ -132,7 +150,7 @@ __device__ __forceinline__ void rope_chunk(const RopeTable& r, int position, con
         unpack_bf16x8(*reinterpret_cast<const uint4*>(row + (second ? 8 * c - half : 8 * c + half)), y);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float2 a = rope_angle(r, position, (second ? 8 * c - half : 8 * c) + i);
+            const auto a = angle((second ? 8 * c - half : 8 * c) + i);
             float p = second ? y[i] : x[i], q = second ? x[i] : y[i];
             rope_turn(p, q, a.x, a.y);
             x[i] = second ? q : p;
@@ -140,7 +158,7 @@ __device__ __forceinline__ void rope_chunk(const RopeTable& r, int position, con
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float2 a = rope_angle(r, position, 4 * c + i);
+            const auto a = angle(4 * c + i);
             rope_turn(x[2 * i], x[2 * i + 1], a.x, a.y);
         }
     }
