@@ -282,6 +282,7 @@ struct WriteArgs {
     int32_t* status;
     RopeTable rope;
     int32_t tokens, hq, hkv, num_pages, num_units;
+    int32_t heads_per_cta;             // cache_write_turned_kernel
     int64_t write_ctas;                // CTAs behind them rotate queries
     int32_t q_shares;                  // shares of the query heads
 };
@@ -356,18 +357,27 @@ __device__ __forceinline__ bool unit_ok(const WriteArgs& a, const int4& u) {
 template <int D>
 __device__ __forceinline__ void rotate_queries(const WriteArgs& a) {
     const int64_t block = (int64_t)blockIdx.x - a.write_ctas;
-    rope_block<D, 2>(a.rope, a.positions, block / a.q_shares * kRopeTokens<D>, a.tokens, 1.f, a.q, a.q, a.out_q, a.out_q, a.hq, a.hq,
-                     4 * (int)(block % a.q_shares), 4 * a.q_shares);
+    rope_block<D, 2>(a.rope, a.positions, block / a.q_shares * kRopeTokens<D>, a.tokens, 1.f, a.q, a.q, a.out_q, a.out_q, a.hq, a.hq, 4 * (int)(block % a.q_shares),
+                     4 * a.q_shares);
 }
 
-// A CTA per unit, KV head and K or V: the rows stay in registers between the look for their largest value and the store, as they
-// came where nothing is rotated (32 registers a thread instead of 64).
-template <int D, bool kFp8, bool kRope>
+template <int kWarps>
+__device__ __forceinline__ uint32_t max_of_warps(uint32_t v, uint32_t* warp_top) {     // of the whole CTA (one barrier)
+    v = __reduce_max_sync(0xffffffffu, v);
+    if ((threadIdx.x & 31) == 0) warp_top[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = warp_top[0];
+#pragma unroll
+    for (int i = 1; i < kWarps; ++i) v = max(v, warp_top[i]);
+    return v;
+}
+
+// A CTA per unit, KV head and K or V: the rows stay in registers, as they came, between the look for their largest value and the store.
+template <int D, bool kFp8>
 __global__ void __launch_bounds__(128) cache_write_pages_kernel(const WriteArgs a) {
     constexpr int kChunks = D / 8, kRows = 128 / kChunks, kPer = kCachePage / kRows;
     __shared__ uint32_t warp_top[4];
     pdl_wait();
-    if (kRope && (int64_t)blockIdx.x >= a.write_ctas) return rotate_queries<D>(a);
     const int which = blockIdx.x & 1, h = (blockIdx.x >> 1) % a.hkv, unit = (blockIdx.x >> 1) / a.hkv;
     const int4 u = a.units[unit];
     if (u.y < 0) return;                                 // behind the last unit
@@ -381,97 +391,151 @@ __global__ void __launch_bounds__(128) cache_write_pages_kernel(const WriteArgs 
     const Rows& in = a.x[which];
     const size_t pitch = (size_t)a.hkv * D;
     const size_t first = ((size_t)u.z * kCachePage) * pitch + (size_t)h * D + 8 * c;     // element of the page's row 0
-    if (!kRope || which == 1) {
-        uint4 x[kPer];
+    uint4 x[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int r = r0 + i * kRows;
+        x[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (r < u.y) x[i] = *reinterpret_cast<const uint4*>(in.at((int64_t)u.x + r, h) + 8 * c);
+    }
+    if constexpr (!kFp8) {
+        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.pages[which]) + first;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int r = r0 + i * kRows;
-            x[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (r < u.y) x[i] = *reinterpret_cast<const uint4*>(in.at((int64_t)u.x + r, h) + 8 * c);
+            if (r < u.y) *reinterpret_cast<uint4*>(out + (u.w + r) * pitch) = x[i];
         }
-        if constexpr (!kFp8) {
-            __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.pages[which]) + first;
+    } else {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) top = magnitude_bits(x[i], top);
+        top = max_of_warps<4>(max(top & 0xffffu, top >> 16), warp_top);
+        const bool finite = top < 0x7f80u;
+        if (!finite) {                                   // once more without what is not (the whole CTA)
+            float most = 0.f;
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
-                const int r = r0 + i * kRows;
-                if (r < u.y) *reinterpret_cast<uint4*>(out + (u.w + r) * pitch) = x[i];
+                float y[8];
+                unpack_bf16x8(x[i], y);
+                most = magnitude_of(y, most);
             }
-        } else {
-            uint32_t top = 0;
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) top = magnitude_bits(x[i], top);
-            top = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));
-            if ((threadIdx.x & 31) == 0) warp_top[threadIdx.x >> 5] = top;
             __syncthreads();
-            top = max(max(warp_top[0], warp_top[1]), max(warp_top[2], warp_top[3]));
-            if (top >= 0x7f80u) {                        // not all finite: once more without those (the whole CTA)
-                float most = 0.f;
+            top = max_of_warps<4>(__float_as_uint(most) >> 16, warp_top);
+        }
+        const float scale = fmaxf(scale_for(__uint_as_float(top << 16)), before), inv = 1.f / scale;
+        uint8_t* out = a.pages[which] + first;
 #pragma unroll
-                for (int i = 0; i < kPer; ++i) {
-                    float y[8];
-                    unpack_bf16x8(x[i], y);
-                    most = magnitude_of(y, most);
-                }
-                __syncthreads();
-                top = __reduce_max_sync(0xffffffffu, __float_as_uint(most) >> 16);
-                if ((threadIdx.x & 31) == 0) warp_top[threadIdx.x >> 5] = top;
-                __syncthreads();
-                top = max(max(warp_top[0], warp_top[1]), max(warp_top[2], warp_top[3])) | 0x80000000u;
+        for (int i = 0; i < kPer; ++i) {
+            const int r = r0 + i * kRows;
+            if (r < u.y) {
+                float y[8];
+                unpack_bf16x8(x[i], y);
+                *reinterpret_cast<uint2*>(out + (u.w + r) * pitch) = finite ? quantize_finite(y, inv) : quantize(y, inv);
             }
-            const bool finite = (top >> 31) == 0;
-            const float scale = fmaxf(scale_for(__uint_as_float(top << 16)), before), inv = 1.f / scale;
-            uint8_t* out = a.pages[which] + first;
+        }
+        finish_page<kRows>(out, pitch, r0, u.w, before, scale, at);
+    }
+}
+
+// The same with a rope, a CTA per unit, K or V, and a few heads: a thread holds the two chunks of eight pairs of a row; the angles of the page are made
+// once, by all threads, for all of the CTA's heads; the next head's rows are on their way while one is written.  (A CTA of 128 threads per head, eight
+// angles to a thread and row: 24000 tokens of 16 / 8 heads 136 us, 77 as it is; a single page of one head 8.6 and 6.6 us.)
+constexpr int kTurnThreads = 256;
+template <int D, bool kFp8>
+__global__ void __launch_bounds__(kTurnThreads) cache_write_turned_kernel(const WriteArgs a) {
+    constexpr int kTasks = D / 16, kRows = kTurnThreads / kTasks, kPer = kCachePage / kRows, kWarps = kTurnThreads / 32;
+    __shared__ uint32_t warp_top[2][kWarps];
+    __shared__ float2 angles[kCachePage][8][kTasks];     // [row][pair of the thread][thread of the row]
+    pdl_wait();
+    const int shares = (a.hkv + a.heads_per_cta - 1) / a.heads_per_cta;
+    const int which = blockIdx.x & 1, h0 = (blockIdx.x >> 1) % shares * a.heads_per_cta, unit = (blockIdx.x >> 1) / shares;
+    const int4 u = a.units[unit];
+    if (u.y < 0) return;                                 // behind the last unit
+    if (!unit_ok(a, u)) {
+        if (threadIdx.x == 0) atomicOr(a.status, BF1_DEV_BAD_ROUTE);
+        return;
+    }
+    const int c = threadIdx.x % kTasks, r0 = threadIdx.x / kTasks, h_end = min(h0 + a.heads_per_cta, a.hkv);
+    const bool turn = which == 0 && 16 * c < a.rope.dim;
+    const int lo = turn && a.rope.half ? 8 * c : 16 * c, hi = turn && a.rope.half ? a.rope.dim / 2 + 8 * c : 16 * c + 8;
+    const Rows& in = a.x[which];
+    uint4 next[kPer][2];
+    auto fetch = [&](int h) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int r = r0 + i * kRows;
+            next[i][0] = next[i][1] = make_uint4(0u, 0u, 0u, 0u);
+            if (r < u.y) {
+                const __nv_bfloat16* row = in.at((int64_t)u.x + r, h);
+                next[i][0] = *reinterpret_cast<const uint4*>(row + lo);
+                next[i][1] = *reinterpret_cast<const uint4*>(row + hi);
+            }
+        }
+    };
+    fetch(h0);
+    if (which == 0) {
+        const int pairs = a.rope.dim / 2;
+#pragma unroll 4
+        for (int i = threadIdx.x; i < u.y * pairs; i += kTurnThreads) {
+            const int r = i / pairs, pair = i - r * pairs;
+            angles[r][pair % 8][pair / 8] = rope_angle(a.rope, a.positions[u.x + r], pair);
+        }
+        __syncthreads();
+    }
+    const size_t pitch = (size_t)a.hkv * D;
+#pragma unroll 1
+    for (int h = h0; h < h_end; ++h) {
+        float* const at = kFp8 ? a.scales[which] + (size_t)u.z * a.hkv + h : nullptr;
+        const float before = kFp8 && u.w > 0 ? *at : 0.f;
+        float x[kPer][2][8], top = 0.f;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            unpack_bf16x8(next[i][0], x[i][0]);
+            unpack_bf16x8(next[i][1], x[i][1]);
+        }
+        if (h + 1 < h_end) fetch(h + 1);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            if (turn && r0 + i * kRows < u.y) {
+                const float2(&by)[8][kTasks] = angles[r0 + i * kRows];
+                if (a.rope.half) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) rope_turn(x[i][0][k], x[i][1][k], by[k][c].x, by[k][c].y);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        rope_turn(x[i][0][2 * k], x[i][0][2 * k + 1], by[k][c].x, by[k][c].y);
+                        rope_turn(x[i][1][2 * k], x[i][1][2 * k + 1], by[4 + k][c].x, by[4 + k][c].y);
+                    }
+                }
+            }
+            if (kFp8) top = magnitude_of(x[i][1], magnitude_of(x[i][0], top));
+        }
+        const size_t first = ((size_t)u.z * kCachePage) * pitch + (size_t)h * D;         // element of the page's row 0
+        if constexpr (!kFp8) {
+            __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.pages[which]) + first;
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
                 const int r = r0 + i * kRows;
                 if (r < u.y) {
-                    float y[8];
-                    unpack_bf16x8(x[i], y);
-                    *reinterpret_cast<uint2*>(out + (u.w + r) * pitch) = finite ? quantize_finite(y, inv) : quantize(y, inv);
+                    *reinterpret_cast<uint4*>(out + (u.w + r) * pitch + lo) = pack_bf16x8(x[i][0]);
+                    *reinterpret_cast<uint4*>(out + (u.w + r) * pitch + hi) = pack_bf16x8(x[i][1]);
                 }
             }
-            finish_page<kRows>(out, pitch, r0, u.w, before, scale, at);
-        }
-        return;
-    }
-    if constexpr (kRope) {
-        float x[kPer][8], top = 0.f;
-        __shared__ float2 angles[kRows][D / 2];
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            if (i * kRows >= u.y) break;
-            __syncthreads();                             // the rows of the round before have been turned
-            for (int j = threadIdx.x; j < kRows * D / 2; j += 128) {
-                const int r = i * kRows + j / (D / 2), pair = j % (D / 2);
-                if (r < u.y && 2 * pair < a.rope.dim) angles[j / (D / 2)][pair] = rope_angle(a.rope, a.positions[u.x + r], pair);
-            }
-            __syncthreads();
-            const int r = r0 + i * kRows;
-            if (r < u.y) {
-                rope_chunk(a.rope, in.at((int64_t)u.x + r, h), c, x[i], [&](int pair) { return angles[r0][pair]; });
-                top = magnitude_of(x[i], top);
-            }
-        }
-        if constexpr (!kFp8) {
-            __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.pages[which]) + first;
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                const int r = r0 + i * kRows;
-                if (r < u.y) *reinterpret_cast<uint4*>(out + (u.w + r) * pitch) = pack_bf16x8(x[i]);
-            }
         } else {
-            const uint32_t bits = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
-            if ((threadIdx.x & 31) == 0) warp_top[threadIdx.x >> 5] = bits;
-            __syncthreads();
-            top = __uint_as_float(max(max(warp_top[0], warp_top[1]), max(warp_top[2], warp_top[3])));
+            // (two places in turn: a warp may be a head ahead of the one that still reads)
+            top = __uint_as_float(max_of_warps<kWarps>(__float_as_uint(top), warp_top[(h - h0) & 1]));
             const float scale = fmaxf(scale_for(top), before), inv = 1.f / scale;
             uint8_t* out = a.pages[which] + first;
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
                 const int r = r0 + i * kRows;
-                if (r < u.y) *reinterpret_cast<uint2*>(out + (u.w + r) * pitch) = quantize(x[i], inv);
+                if (r < u.y) {
+                    *reinterpret_cast<uint2*>(out + (u.w + r) * pitch + lo) = quantize(x[i][0], inv);
+                    *reinterpret_cast<uint2*>(out + (u.w + r) * pitch + hi) = quantize(x[i][1], inv);
+                }
             }
-            finish_page<kRows>(out, pitch, r0, u.w, before, scale, at);
+            finish_page<kTurnThreads / (D / 8)>(out + 8 * (threadIdx.x % (D / 8)), pitch, threadIdx.x / (D / 8), u.w, before, scale, at);
         }
     }
 }
@@ -609,9 +673,12 @@ extern "C" int bf1_plan_cache(const int32_t* seqlens_dev, const int32_t* new_len
     a.max_pages = max_pages_per_seq;
     a.num_pages = num_pages;
     a.p = *out;
-    // one CTA for what 1024 threads do in a few rounds
+    // one CTA for what its threads do in a few rounds
     const int ctas = out->capacity_tokens <= 8192 && out->batch <= kTableThreads ? 1 : 8;
-    const int threads = ctas == 1 && out->batch <= 128 && out->capacity_tokens <= 512 ? 128 : kTableThreads;
+    // us with 128 / 256 / 512 / 1024 threads: 120 sequences of a token 3.6 / 3.7 / 4.1 / 5.2, 26 of 22 4.6 / 4.3 / 4.6 / 5.5, 240 of a token 5.2 / 4.1 /
+    // 4.4 / 5.5, of 30 9.6 / 6.5 / 6.2 / 7.1, 600 of a token 10.6 / 7.4 / 6.6 / 6.4
+    const int threads = ctas > 1 || out->batch > 512 ? kTableThreads
+                        : out->batch > 256 || out->capacity_tokens > 4096 ? 512 : out->batch > 128 || out->capacity_tokens > 512 ? 256 : 128;
     BF1_CUDA_CHECK(launch_pdl_cluster(plan_cache_kernel, dim3(ctas), dim3(ctas), threads, 0, (cudaStream_t)stream, a));
     return BF1_OK;
 }
@@ -654,21 +721,33 @@ extern "C" int bf1_cache_write(const bf1_rows* k, const bf1_rows* v, const bf1_r
     a.hq = hq;
     a.hkv = hkv;
     a.num_pages = num_pages;
-#define BF1_WRITE(kernel, rope) {{kernel<64, false, rope>, kernel<128, false, rope>}, {kernel<64, true, rope>, kernel<128, true, rope>}}
-    static const WriteKernel kernels[2][2][2][2] = {   // [few tokens to a unit][a rope][8 bits][d = 128]
-        {BF1_WRITE(cache_write_pages_kernel, false), BF1_WRITE(cache_write_pages_kernel, true)},
-        {BF1_WRITE(cache_write_tokens_kernel, false), BF1_WRITE(cache_write_tokens_kernel, true)}};
-#undef BF1_WRITE
-    const bool few = tokens < 8 * (int64_t)plan->batch;
+    static const WriteKernel tokens_kernels[2][2][2] = {   // [a rope][8 bits][d = 128]
+        {{cache_write_tokens_kernel<64, false, false>, cache_write_tokens_kernel<128, false, false>},
+         {cache_write_tokens_kernel<64, true, false>, cache_write_tokens_kernel<128, true, false>}},
+        {{cache_write_tokens_kernel<64, false, true>, cache_write_tokens_kernel<128, false, true>},
+         {cache_write_tokens_kernel<64, true, true>, cache_write_tokens_kernel<128, true, true>}}};
+    static const WriteKernel pages_kernels[2][2][2] = {
+        {{cache_write_pages_kernel<64, false>, cache_write_pages_kernel<128, false>}, {cache_write_pages_kernel<64, true>, cache_write_pages_kernel<128, true>}},
+        {{cache_write_turned_kernel<64, false>, cache_write_turned_kernel<128, false>}, {cache_write_turned_kernel<64, true>, cache_write_turned_kernel<128, true>}}};
+    const bool few = tokens < 8 * (int64_t)plan->batch, turned = rope != nullptr;
     const int64_t units = bf1_cache_plan_units(plan->batch, tokens);
     if (plan->capacity_units < units) return fail(BF1_ERR_CAPACITY, "cache plan capacity_units %d < %d", plan->capacity_units, (int)units);
     a.num_units = (int32_t)units;
-    a.write_ctas = few ? (units * hkv + 3) / 4 : units * hkv * 2;
-    const int per_cta = d == 128 ? kRopeTokens<128> : kRopeTokens<64>;
-    const int64_t token_ctas = ((int64_t)tokens + per_cta - 1) / per_cta;
-    a.q_shares = hq ? (int)std::max<int64_t>(1, std::min<int64_t>((hq + 3) / 4, 148 * 8 / token_ctas)) : 0;
+    // heads that share their angles: as many as leave three CTAs for every SM
+    a.heads_per_cta = (int)std::max<int64_t>(1, std::min<int64_t>(hkv, units * 2 * hkv / (3 * 148)));
+    a.write_ctas = few ? (units * hkv + 3) / 4 : turned ? units * 2 * ((hkv + a.heads_per_cta - 1) / a.heads_per_cta) : units * 2 * hkv;
+    int64_t token_ctas = 0;
+    a.q_shares = 0;
+    if (hq && few) {
+        const int per_cta = d == 128 ? kRopeTokens<128> : kRopeTokens<64>;
+        token_ctas = ((int64_t)tokens + per_cta - 1) / per_cta;
+        a.q_shares = (int)std::max<int64_t>(1, std::min<int64_t>((hq + 3) / 4, 148 * 8 / token_ctas));
+    } else if (hq) {   // a launch of their own: beside the writes they would have those CTAs' registers (18000 tokens of one head 24 us, 22 as it is)
+        if (int rc = bf1_rope_fwd(q, nullptr, plan->positions, tokens, hq, 0, d, rope, out_q, nullptr, stream)) return rc;
+    }
     const int64_t ctas = a.write_ctas + token_ctas * a.q_shares;
     if (ctas > 0x7fffffffLL) return fail(BF1_ERR_UNSUPPORTED, "%d tokens of %d query and %d KV heads in one call", tokens, hq, hkv);
-    BF1_CUDA_CHECK(launch_pdl(kernels[few][rope != nullptr][k_scales != nullptr][d == 128], dim3((unsigned)ctas), 128, 0, (cudaStream_t)stream, a));
+    BF1_CUDA_CHECK(launch_pdl((few ? tokens_kernels : pages_kernels)[turned][k_scales != nullptr][d == 128], dim3((unsigned)ctas),
+                              !few && turned ? kTurnThreads : 128, 0, (cudaStream_t)stream, a));
     return BF1_OK;
 }

@@ -254,7 +254,7 @@ struct Merge8 {                          // the four warps' states at the end of
 
 // grid (hkv, runs), (hkv, batch) or (hkv, batch, CTAs of the cluster)
 template <int D, int kHeads, int kMode>
-__global__ void __launch_bounds__(kD8Threads, kMode == kRuns ? 3 : 2) decode8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+__global__ void __launch_bounds__(kD8Threads, kMode == kWhole ? 2 : 3) decode8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                                                                 const Decode8Args a) {
     constexpr int kPageBytes = kP8 * D;
     extern __shared__ uint8_t dsmem[];
@@ -769,17 +769,18 @@ extern "C" int bf1_decode_fwd_fp8(const void* q, const void* k_pages, const void
     const int64_t lists = (int64_t)batch * hkv;
     const int most = plan->max_degree;
     auto ceil_div = [](int64_t x, int64_t y) { return (int)((x + y - 1) / y); };
-    // Which way, by what the host knows: the number of lists and the longest that there may be.  Over 574 shapes (1 to 1120 lists of up to 1
-    // to 400 pages, d = 64 and 128, two and four heads, lists alike or of all lengths up to the longest, on pages that no cache holds) this
-    // takes 0.9 % longer on average than the best of the three, 24 % at most.  us in runs / whole / in parts (16 query / 8 KV heads, d = 128):
+    // Which way, by what the host knows: the number of lists and the longest that there may be.  Over 796 shapes (1 to 1120 lists of up to 1
+    // to 400 pages, d = 64 and 128, two and four heads; lists alike, from short to the longest evenly, and mostly short ones; on pages that no cache
+    // holds) this takes 2.2 % longer on average than the best of the three, mostly where one list is far longer than the others.  us in
+    // runs / whole / in parts (16 query / 8 KV heads, d = 128):
     //   up to two pages a cluster never pays: one sequence of 1 / 2 pages 2.9 / 3.3 whole, 4.1 / 3.9 in parts;
-    //   lists for every SM: 32 sequences of 12 pages 19.2 / 12.2 / 13.9, 140 of 24 unlike ones 58 / 58 / 52, of 48 88 / 105 / 87, 32 alike of 48
-    //     40.8 / 34.6 / 37.7 and unlike ones of 100 43 / 52 / 58;
-    //   fewer: one sequence of 12 / 64 / 200 / 400 pages 9.2 / 7.4 / 4.4, 12.1 / 29 / 8.2, 15.4 / 84 / 13.0, 19.7 / 164 / 20.0, 14 unlike ones
-    //     of 64 / 100 / 200 pages 20.5 / 30 / 22.4, 25.3 / 44 / 31.6, 39.5 / 84 / 56.5.
+    //   lists for every SM: 32 sequences of 12 pages 19.5 / 12.9 / 14.6, 140 of 4 27 / 25 / 26, 32 alike of 48 40 / 34 / 38, 64 of 48 71 / 87 / 83,
+    //     64 of up to 48, mostly short, 26 / 39 / 30;
+    //   fewer: one sequence of 12 / 48 / 200 / 400 pages 9.2 / 7.3 / 4.4, 11.7 / 23 / 7.5, 15.4 / 84 / 13.3, 19.7 / 164 / 20.0, eight of 48 / 200
+    //     18.6 / 23 / 14.3, 41 / 85 / 38, of up to 200, mostly short, 20.9 / 83 / 21.7.
     int mode = kRuns;
     if (batch > kD8MaxScan || most <= 2 || (lists >= sms && most <= 24)) mode = kWhole;
-    else if (lists < sms && most <= 400 && most * lists <= 10000) mode = kParts;
+    else if (lists < sms && most <= 400 && most * lists <= 14000) mode = kParts;
     a.runs = a.nctas = a.share = 0;
     size_t smem = 1024;
     if (mode == kRuns) {

@@ -24,11 +24,12 @@ struct RopeArgs {
 };
 
 // blockIdx.x: tokens; blockIdx.y: one of gridDim.y shares of the heads
-template <int D>
+template <int D, int kSplit>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs a) {
+    constexpr int kWarps = kSplit > 1 ? 1 : 4;           // that share the heads
     pdl_wait();
-    rope_block<D, kRopeAhead>(a.rope, a.positions, (int64_t)blockIdx.x * kRopeTokens<D>, a.tokens, a.sign, a.q, a.k, a.out_q, a.out_k, a.hq, a.heads,
-                              4 * blockIdx.y, 4 * gridDim.y);
+    rope_block<D, kRopeAhead, kSplit>(a.rope, a.positions, (int64_t)blockIdx.x * kRopeTokens<D, kSplit>, a.tokens, a.sign, a.q, a.k, a.out_q, a.out_k,
+                                      a.hq, a.heads, kWarps * blockIdx.y, kWarps * gridDim.y);
 }
 
 int check_rows(const bf1_rows* rows, const char* name) {
@@ -73,10 +74,14 @@ static int rope_call(const bf1_rows* q, const bf1_rows* k, const int32_t* positi
     a.hq = hq;
     a.heads = hq + hkv;
     a.sign = sign;
-    // few tokens: their heads are shared out, four at least to a CTA
-    const int ctas = d == 128 ? (tokens + kRopeTokens<128> - 1) / kRopeTokens<128> : (tokens + kRopeTokens<64> - 1) / kRopeTokens<64>;
-    const int shares = std::max(1, std::min((a.heads + 3) / 4, 148 * 8 / ctas));
-    BF1_CUDA_CHECK(launch_pdl(d == 128 ? rope_kernel<128> : rope_kernel<64>, dim3(ctas, shares), kRopeThreads, 0, (cudaStream_t)stream, a));
+    // Fewer than four heads: a warp for each would leave the others without (with the write of a cache behind it, 18000 tokens of one head 22 us, 16 with
+    // tokens of its own for each warp).
+    // Few tokens: their heads are shared out among CTAs.
+    static void (*const kernels[2][2])(RopeArgs) = {{rope_kernel<64, 1>, rope_kernel<128, 1>}, {rope_kernel<64, 4>, rope_kernel<128, 4>}};
+    const bool split = a.heads < 4;
+    const int per_cta = (d == 128 ? kRopeTokens<128> : kRopeTokens<64>) * (split ? 4 : 1), ctas = (tokens + per_cta - 1) / per_cta;
+    const int shares = split ? 1 : std::max(1, std::min((a.heads + 3) / 4, 148 * 8 / ctas));
+    BF1_CUDA_CHECK(launch_pdl(kernels[split][d == 128], dim3(ctas, shares), kRopeThreads, 0, (cudaStream_t)stream, a));
     return BF1_OK;
 }
 

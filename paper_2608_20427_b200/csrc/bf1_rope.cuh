@@ -68,23 +68,26 @@ struct Rows {
     __device__ __forceinline__ __nv_bfloat16* at(int64_t token, int h) const { return p + token * row + h * head; }
 };
 
-// What a CTA of 128 threads does: kRopeTokens tokens (from `token0`), a lane to sixteen dimensions of one, and for each warp the heads h0 + warp, h0 + warp +
-// step, ...: the eight pairs 8 c .. 8 c + 7, or sixteen dimensions that are carried over.  The angles of the tokens are made once, two to a
-// thread, and handed out through shared memory (each thread making its own eight: 4096 tokens of 24 heads 12.1 us, 9.9 as it is).  kAhead heads are asked for
-// before the first is turned.  sign -1 turns back, which is the gradient (a rotation's transpose; the magnitude stays).
+// What a CTA of 128 threads does: kRopeTokens tokens from `token0`, a lane to sixteen dimensions of one, and for each warp the heads h0 + warp, h0 + warp +
+// step, ...: the eight pairs 8 c .. 8 c + 7, or sixteen dimensions that are carried over.  The angles of the tokens are made once, two to a thread, and
+// handed out through shared memory (each thread making its own eight: 4096 tokens of 24 heads 12.1 us, 9.9 as it is).  kAhead heads are asked for before
+// the first is turned.  sign -1 turns back, which is the gradient (a rotation's transpose; the magnitude stays).  With kSplit = 4 every warp has
+// tokens of its own and all the heads, of which there are fewer than four then.
 constexpr int kRopeThreads = 128;
-template <int D>
-constexpr int kRopeTokens = 32 / (D / 16);
-template <int D, int kAhead>
+template <int D, int kSplit = 1>
+constexpr int kRopeTokens = kSplit * 32 / (D / 16);
+template <int D, int kAhead, int kSplit = 1>
 __device__ __forceinline__ void rope_block(const RopeTable& r, const int32_t* positions, int64_t token0, int tokens, float sign, const Rows& in_q,
                                            const Rows& in_k, const Rows& out_q, const Rows& out_k, int hq, int heads, int h0, int step) {
     constexpr int kLanes = D / 16;                       // to a token
-    __shared__ float2 angles[kRopeTokens<D>][8][kLanes]; // [token][pair of the lane][lane]
-    for (int i = threadIdx.x; i < kRopeTokens<D> * kLanes * 8; i += kRopeThreads) {
+    constexpr int kTokens = kRopeTokens<D, kSplit>;
+    __shared__ float2 angles[kTokens][8][kLanes];        // [token][pair of the lane][lane]
+    const int warp = threadIdx.x >> 5;
+    for (int i = threadIdx.x; i < kTokens * kLanes * 8; i += kRopeThreads) {
         const int t = i / (kLanes * 8), pair = i % (kLanes * 8);
         if (2 * pair < r.dim && token0 + t < tokens) angles[t][pair % 8][pair / 8] = rope_angle(r, positions[token0 + t], pair);
     }
-    const int lane = threadIdx.x & 31, t = lane / kLanes, c = lane % kLanes;
+    const int lane = threadIdx.x & 31, t = (kSplit > 1 ? warp * (32 / kLanes) : 0) + lane / kLanes, c = lane % kLanes;
     const int64_t token = token0 + t;
     const bool live = token < tokens && positions[token] >= 0;   // padding: its rows stay as they are
     __syncthreads();
@@ -100,7 +103,7 @@ __device__ __forceinline__ void rope_block(const RopeTable& r, const int32_t* po
             sn[i] = a.y * sign;
         }
     }
-    for (int h = h0 + (threadIdx.x >> 5); h < heads; h += kAhead * step) {
+    for (int h = kSplit > 1 ? h0 : h0 + warp; h < heads; h += kAhead * step) {
         uint4 a[kAhead], b[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
