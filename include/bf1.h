@@ -353,7 +353,8 @@ int bf1_rope_turns(const bf1_rope_cfg *cfg /* host */, double *turns /* host out
 
 /* Rotates the hq query heads and hkv key heads of `tokens` tokens (hkv = 0: there are no keys; k and out_k are not read).
  *   positions_dev  device int32 [tokens]; a token of negative position is padding: its output rows are not written
- *   out_q, out_k   the inputs themselves (same data, same strides) or rows that do not overlap them
+ *   out_q, out_k   the inputs themselves (same data, same strides) or rows that do not overlap them; rows of one output, and the
+ *                  two outputs, do not overlap either
  * bf1_rope_bwd takes the gradients of the rotated heads and gives those of the heads before the rotation. */
 int bf1_rope_fwd(const bf1_rows *q, const bf1_rows *k, const int32_t *positions_dev, int32_t tokens, int32_t hq, int32_t hkv,
                  int32_t d, const bf1_rope *rope /* host */, const bf1_rows *out_q, const bf1_rows *out_k, void *stream);

@@ -410,7 +410,7 @@ class Rope:
         """A rope of the caller's own frequencies: `turns` of a pair per position (radians / 2 pi), [dim / 2]."""
         if layout not in ROPE_LAYOUTS:
             raise ValueError("layout %r: one of %s" % (layout, ", ".join(ROPE_LAYOUTS)))
-        turns = torch.as_tensor(turns, dtype=torch.float64).to(device).contiguous()
+        turns = torch.as_tensor(turns, dtype=torch.float64).to(device, copy=True).contiguous()
         if turns.dim() != 1 or turns.numel() < 8 or turns.numel() % 8:
             raise ValueError("turns must be 1-d, 8 pairs at a time")
         r = Rope(2 * turns.numel(), layout, float(magnitude), turns)

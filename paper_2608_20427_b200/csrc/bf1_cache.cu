@@ -540,82 +540,100 @@ __global__ void __launch_bounds__(kTurnThreads) cache_write_turned_kernel(const 
     }
 }
 
-// A warp per unit and KV head, half of it for K and half for V: for units of a token or a few, which a CTA would not fill.
+// A CTA per unit and four KV heads, a warp to each, half of it for K and half for V: for units of a token or a few, which a CTA would not fill.  kDeep rows
+// (twice as many with d = 64) are on their way at once, under angles that the whole CTA makes; a longer unit's rows are read twice, for the scale and
+// for the store.
 template <int D, bool kFp8, bool kRope>
 __global__ void __launch_bounds__(128) cache_write_tokens_kernel(const WriteArgs a) {
-    constexpr int kChunks = D / 8, kRows = 16 / kChunks;        // lanes to a row, rows at a time
+    constexpr int kChunks = D / 8, kRows = 16 / kChunks, kDeep = 2, kRound = kDeep * kRows;    // lanes to a row, rows side by side and in a round
     pdl_wait();
     if (kRope && (int64_t)blockIdx.x >= a.write_ctas) return rotate_queries<D>(a);
-    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-    const int unit = (int)(item / a.hkv), h = (int)(item % a.hkv);
-    if (unit >= a.num_units) return;                            // (the last CTA may have warps to spare)
+    const int groups = (a.hkv + 3) / 4, unit = blockIdx.x / groups, h = blockIdx.x % groups * 4 + (threadIdx.x >> 5);
+    const bool live = h < a.hkv;
     const int4 u = a.units[unit];
     if (u.y < 0) return;                                        // behind the last unit
     const int lane = threadIdx.x & 31, which = lane >> 4, c = lane % kChunks, r0 = (lane & 15) / kChunks;
     if (!unit_ok(a, u)) {
-        if (lane == 0) atomicOr(a.status, BF1_DEV_BAD_ROUTE);
+        if (threadIdx.x == 0) atomicOr(a.status, BF1_DEV_BAD_ROUTE);
         return;
     }
     const Rows& in = a.x[which];
-    // the angles of kRows rows, D / 2 pairs to each: two to a lane, in 64 bits where numbers in 8 bits come of them
+    // The angles, D / 2 pairs to a row: of one round, in 64 bits where numbers in 8 bits come of them, or, where there are more rounds, of all rows at once in
+    // 32 bits (a round's angles in front of every round: four prompts of 120 among 512 sequences 140 us, 62 as it is)
     using Angle = typename std::conditional<kFp8, double2, float2>::type;
-    __shared__ Angle angles[kRope ? 4 : 1][kRope ? 64 : 1];
-    auto turn_rows = [&](int rb) {
-        if constexpr (kRope) {
-            __syncwarp();
+    __shared__ __align__(16) uint8_t angle_bytes[kRope ? kCachePage * D / 2 * sizeof(float2) : 16];
+    static_assert(!kRope || sizeof(Angle) * kRound <= sizeof(float2) * kCachePage, "a round's angles are no more than a page's");
+    Angle* const round_angles = reinterpret_cast<Angle*>(angle_bytes);
+    float2* const page_angles = reinterpret_cast<float2*>(angle_bytes);
+    const bool rounds = u.y > kRound;
+    if constexpr (kRope) {
+        for (int i = threadIdx.x; i < u.y * D / 2; i += 128) {
+            const int r = i / (D / 2), pair = i % (D / 2);
+            if (2 * pair >= a.rope.dim) continue;
+            if (rounds || !kFp8) page_angles[i] = rope_angle(a.rope, a.positions[u.x + r], pair);
+            else if constexpr (kFp8) round_angles[i] = rope_angle64(a.rope, a.positions[u.x + r], pair);
+        }
+        __syncthreads();
+    }
+    float x[kDeep][8];                                          // rows rb + r0, rb + r0 + kRows, ...
+    const bool turn = kRope && which == 0 && 8 * c < a.rope.dim;
+    const int other = turn && a.rope.half ? 8 * rope_other(a.rope, c) : 8 * c;
+    auto load = [&](int rb) {                                   // (all loads in front of what K and V do apart)
+        uint4 own[kDeep], pair_of[kDeep];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int i = lane + 32 * j, r = rb + i / (D / 2), pair = i % (D / 2);
-                if (r < u.y && 2 * pair < a.rope.dim) {
-                    if constexpr (kFp8) angles[threadIdx.x >> 5][i] = rope_angle64(a.rope, a.positions[u.x + r], pair);
-                    else angles[threadIdx.x >> 5][i] = rope_angle(a.rope, a.positions[u.x + r], pair);
-                }
-            }
-            __syncwarp();
+        for (int j = 0; j < kDeep; ++j) {
+            const int r = rb + r0 + j * kRows;
+            own[j] = pair_of[j] = make_uint4(0u, 0u, 0u, 0u);
+            if (!live || r >= u.y) continue;
+            const __nv_bfloat16* row = in.at((int64_t)u.x + r, h);
+            own[j] = *reinterpret_cast<const uint4*>(row + 8 * c);
+            if (kRope) pair_of[j] = *reinterpret_cast<const uint4*>(row + other);
         }
-    };
-    auto load = [&](int r, float (&x)[8]) {
-        const __nv_bfloat16* row = in.at((int64_t)u.x + r, h);
-        if constexpr (kRope) {
-            if (which == 0) return rope_chunk(a.rope, row, c, x, [&](int pair) { return angles[threadIdx.x >> 5][r0 * (D / 2) + pair]; });
+#pragma unroll
+        for (int j = 0; j < kDeep; ++j) {
+            const int r = rb + r0 + j * kRows;
+            unpack_bf16x8(own[j], x[j]);
+            if (!turn || r >= u.y) continue;
+            if (rounds) rope_chunk(a.rope, c, x[j], pair_of[j], [&](int pair) { return page_angles[r * (D / 2) + pair]; });
+            else rope_chunk(a.rope, c, x[j], pair_of[j], [&](int pair) { return round_angles[r * (D / 2) + pair]; });
         }
-        unpack_bf16x8(*reinterpret_cast<const uint4*>(row + 8 * c), x);
     };
     const size_t pitch = (size_t)a.hkv * D;
     const size_t first = ((size_t)u.z * kCachePage) * pitch + (size_t)h * D + 8 * c;
-    float x[8];
     if constexpr (!kFp8) {
         __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.pages[which]) + first;
-        for (int rb = 0; rb < u.y; rb += kRows) {
-            turn_rows(rb);
-            if (rb + r0 < u.y) {
-                load(rb + r0, x);
-                *reinterpret_cast<uint4*>(out + (u.w + rb + r0) * pitch) = pack_bf16x8(x);
+        for (int rb = 0; rb < u.y; rb += kRound) {
+            load(rb);
+#pragma unroll
+            for (int j = 0; j < kDeep; ++j) {
+                const int r = rb + r0 + j * kRows;
+                if (live && r < u.y) *reinterpret_cast<uint4*>(out + (u.w + r) * pitch) = pack_bf16x8(x[j]);
             }
         }
         return;
     }
     float* const at = a.scales[which] + (size_t)u.z * a.hkv + h;
-    const float before = u.w > 0 ? *at : 0.f;
+    const float before = live && u.w > 0 ? *at : 0.f;
     float top = 0.f;
-    for (int rb = (u.y - 1) / kRows * kRows; rb >= 0; rb -= kRows) {       // the first rows last: they stay in x
-        turn_rows(rb);
-        if (rb + r0 < u.y) {
-            load(rb + r0, x);
-            top = magnitude_of(x, top);
-        }
+    for (int rb = (u.y - 1) / kRound * kRound; rb >= 0; rb -= kRound) {    // the first rows last: they stay in x
+        load(rb);
+#pragma unroll
+        for (int j = 0; j < kDeep; ++j)
+            if (live && rb + r0 + j * kRows < u.y) top = magnitude_of(x[j], top);
     }
 #pragma unroll
     for (int off = 8; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
     const float scale = fmaxf(scale_for(top), before), inv = 1.f / scale;
     uint8_t* out = a.pages[which] + first;
-    for (int rb = 0; rb < u.y; rb += kRows) {
-        if (rb > 0) turn_rows(rb);
-        if (rb + r0 < u.y) {
-            if (rb > 0) load(rb + r0, x);
-            *reinterpret_cast<uint2*>(out + (u.w + rb + r0) * pitch) = quantize(x, inv);
+    for (int rb = 0; rb < u.y; rb += kRound) {
+        if (rb > 0) load(rb);
+#pragma unroll
+        for (int j = 0; j < kDeep; ++j) {
+            const int r = rb + r0 + j * kRows;
+            if (live && r < u.y) *reinterpret_cast<uint2*>(out + (u.w + r) * pitch) = quantize(x[j], inv);
         }
     }
+    if (!live) return;
     if (u.w > 0 && before != scale) {
         constexpr int kAhead = 8;
         for (int r = r0; r < u.w; r += kAhead * kRows) {
@@ -729,13 +747,16 @@ extern "C" int bf1_cache_write(const bf1_rows* k, const bf1_rows* v, const bf1_r
     static const WriteKernel pages_kernels[2][2][2] = {
         {{cache_write_pages_kernel<64, false>, cache_write_pages_kernel<128, false>}, {cache_write_pages_kernel<64, true>, cache_write_pages_kernel<128, true>}},
         {{cache_write_turned_kernel<64, false>, cache_write_turned_kernel<128, false>}, {cache_write_turned_kernel<64, true>, cache_write_turned_kernel<128, true>}}};
-    const bool few = tokens < 8 * (int64_t)plan->batch, turned = rope != nullptr;
+    // Few tokens to a sequence, as far as the host knows: a warp to a unit and head, which shares a CTA's angles with three others.  us, so / a CTA to a unit
+    // (16 / 8 heads, d = 128, 8 bits, rotated on the way): 256 sequences of one token 4.0 / 5.7, of two 6.1 / 17.1, of four 15.1 / 22.6, eight of four 6.5 / 4.2,
+    // of seven 11.3 / 4.5; 508 of one and four of 120 62 / 32, 480 of one and 32 of 100 177 / 43.
+    const bool few = tokens <= 2 * (int64_t)plan->batch, turned = rope != nullptr;
     const int64_t units = bf1_cache_plan_units(plan->batch, tokens);
     if (plan->capacity_units < units) return fail(BF1_ERR_CAPACITY, "cache plan capacity_units %d < %d", plan->capacity_units, (int)units);
     a.num_units = (int32_t)units;
     // heads that share their angles: as many as leave three CTAs for every SM
     a.heads_per_cta = (int)std::max<int64_t>(1, std::min<int64_t>(hkv, units * 2 * hkv / (3 * 148)));
-    a.write_ctas = few ? (units * hkv + 3) / 4 : turned ? units * 2 * ((hkv + a.heads_per_cta - 1) / a.heads_per_cta) : units * 2 * hkv;
+    a.write_ctas = few ? units * ((hkv + 3) / 4) : turned ? units * 2 * ((hkv + a.heads_per_cta - 1) / a.heads_per_cta) : units * 2 * hkv;
     int64_t token_ctas = 0;
     a.q_shares = 0;
     if (hq && few) {

@@ -117,6 +117,11 @@ bf1_rows rows_of(const at::Tensor& t, const at::Tensor& like, const char* what) 
     require(t.device() == like.device() && t.scalar_type() == at::kBFloat16 && t.dim() == 3 && (t.size(2) == 1 || t.stride(2) == 1), what);
     return {t.data_ptr(), t.size(0) > 1 ? t.stride(0) : 0, t.size(1) > 1 ? t.stride(1) : 0};
 }
+// The same for a result: its rows and heads each have a place of their own.
+bf1_rows result_rows(const at::Tensor& t, const at::Tensor& like, const char* what) {
+    require((t.size(0) < 2 || t.stride(0) != 0) && (t.size(1) < 2 || t.stride(1) != 0), "an output's rows must not share memory");
+    return rows_of(t, like, what);
+}
 template <typename T>
 T* array_of(const at::Tensor& t, const at::Tensor& like, at::ScalarType type, const char* what) {
     require(t.device() == like.device() && t.scalar_type() == type && t.is_contiguous(), what);
@@ -302,7 +307,7 @@ PyObject* rope(PyObject* const* a) {
         out_k = !keys ? out_q : a[7] == Py_None ? fresh(k.sizes(), q, at::kBFloat16) : tensor(a[7]);
     }
     require(out_q.sizes() == q.sizes() && out_k.sizes() == (keys ? k : q).sizes(), "the outputs must have the shapes of q and k");
-    const bf1_rows oq = rows_of(out_q, q, what), ok = rows_of(out_k, q, what);
+    const bf1_rows oq = result_rows(out_q, q, what), ok = result_rows(out_k, q, what);
     const int32_t tokens = q.size(0), hq = q.size(1), hkv = keys ? k.size(1) : 0, d = q.size(2);
     call([&] {
         return back ? bf1_rope_bwd(&qr, &kr, pp, tokens, hq, hkv, d, table, &oq, &ok, place.stream)
@@ -384,7 +389,7 @@ PyObject* cache_write(PyObject* const* a) {
         require(q.size(0) == k.size(0) && q.size(2) == k.size(2), "q and k must have the same tokens and head dimension");
         out_q = a[11] == Py_None ? at::empty(q.sizes(), q.options()) : tensor(a[11]);
         require(out_q.sizes() == q.sizes(), "out_q must have the shape of q");
-        oq = rows_of(out_q, k, what);
+        oq = result_rows(out_q, k, what);
         hq = q.size(1);
     }
     const int32_t tokens = k.size(0), hkv = k.size(1), d = k.size(2), pages = kp.size(0);

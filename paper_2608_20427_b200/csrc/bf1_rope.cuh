@@ -141,19 +141,19 @@ __device__ __forceinline__ void rope_block(const RopeTable& r, const int32_t* po
     }
 }
 
-// Dimensions 8 c .. 8 c + 7 of a row, rotated by angle(pair) = (cos, sin).
+// Dimensions 8 c .. 8 c + 7 of a row, rotated by angle(pair) = (cos, sin), in place of x.  With pairs of halves `other` are the eight dimensions that
+// they are paired with, 8 rope_other(r, c) and up.
+__device__ __forceinline__ int rope_other(const RopeTable& r, int c) { return 16 * c < r.dim ? c + r.dim / 16 : c - r.dim / 16; }
 template <typename F>
-__device__ __forceinline__ void rope_chunk(const RopeTable& r, const __nv_bfloat16* row, int c, float (&x)[8], F&& angle) {
-    unpack_bf16x8(*reinterpret_cast<const uint4*>(row + 8 * c), x);
-    if (8 * c >= r.dim) return;
+__device__ __forceinline__ void rope_chunk(const RopeTable& r, int c, float (&x)[8], const uint4& other, F&& angle) {
     if (r.half) {
-        const int half = r.dim / 2;
-        const bool second = 8 * c >= half;
+        const bool second = 16 * c >= r.dim;
+        const int pair = second ? 8 * c - r.dim / 2 : 8 * c;
         float y[8];
-        unpack_bf16x8(*reinterpret_cast<const uint4*>(row + (second ? 8 * c - half : 8 * c + half)), y);
+        unpack_bf16x8(other, y);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const auto a = angle((second ? 8 * c - half : 8 * c) + i);
+            const auto a = angle(pair + i);
             float p = second ? y[i] : x[i], q = second ? x[i] : y[i];
             rope_turn(p, q, a.x, a.y);
             x[i] = second ? q : p;

@@ -197,7 +197,7 @@ def check_write(got, before, x, plan, scales=None, scales_before=None, exact_inp
 
 
 WRITES = [([0], [1]), ([63], [1]), ([64], [1]), ([10, 0, 127, 64, 31], [1, 1, 1, 0, 1]), ([0, 61, 64, 5], [64, 6, 129, 200]), ([3, 3], [2, 5]), ([1], [63]),
-          ([0] * 40, [1] * 40)]
+          ([0] * 40, [1] * 40), ([61] + [9] * 39, [55] + [0] * 20 + [1] * 19)]
 
 
 @pytest.mark.parametrize("fp8", [True, False], ids=["e4m3", "bf16"])
@@ -206,7 +206,7 @@ WRITES = [([0], [1]), ([63], [1]), ([64], [1]), ([10, 0, 127, 64, 31], [1, 1, 1,
 def test_write(lens, new, hkv, d, fp8):
     g = torch.Generator().manual_seed(sum(lens) + hkv + d)
     rng = np.random.default_rng(5)
-    tokens, pages = sum(new) + 3, 60
+    tokens, pages = sum(new) + 3, 60 + len(lens)
     table_in, free = tables(lens, pages, 8, rng)
     plan = bf1.plan_cache(ints(lens), ints(new), ints(table_in), pages, tokens, stack_of(free, pages), ints([len(free)]))
     # sizes all over the place, so that scales of partial pages have to grow, or stay
@@ -223,6 +223,21 @@ def test_write(lens, new, hkv, d, fp8):
     now = [None if t is None else t.clone() for t in (kp, vp, ks, vs)]
     bf1.cache_write(k.to(DEV), v.to(DEV), kp, vp, plan, ks, vs)   # the same once more changes nothing
     assert all(x is None or torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(now, (kp, vp, ks, vs)))
+
+
+def test_a_refused_step_writes_nothing():
+    """Its plan has no units and no positions: pages, scales and rotated queries stay as they are."""
+    g = torch.Generator().manual_seed(3)
+    rope = bf1.plan_rope(bf1.RopeCfg(64), DEV)
+    for tokens in (3, 40):                                          # both kernels
+        kp, vp, ks, vs = cache(4, 2, 64, True, g)
+        was = [t.clone() for t in (kp, vp, ks, vs)]
+        plan = bf1.plan_cache(ints([0, 0, 0]), ints([1, 1, 1000]), ints([[0], [1], [2]]), 4, tokens)
+        assert plan.status.item() & 1
+        k = torch.ones((tokens, 2, 64), dtype=torch.bfloat16, device=DEV)
+        out = torch.full_like(k, 5.0)
+        bf1.cache_write(k, k, kp, vp, plan, ks, vs, rope=rope, q=k, out_q=out)
+        assert out.eq(5).all() and all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(was, (kp, vp, ks, vs)))
 
 
 def test_scales_grow_token_by_token_as_for_the_whole_page():
@@ -265,10 +280,12 @@ def test_values_that_are_not_finite_and_zeros(many):
 
 @pytest.mark.parametrize("fp8", [True, False], ids=["e4m3", "bf16"])
 @pytest.mark.parametrize("layout,dim,d,hq,hkv", [("half", 128, 128, 16, 8), ("half", 48, 64, 3, 1), ("interleaved", 64, 64, 8, 2), ("interleaved", 32, 128, 5, 5)])
-@pytest.mark.parametrize("lens,new", [([5, 1000, 63], [1, 1, 1]), ([100, 0], [90, 70])], ids=["tokens", "prompts"])
+@pytest.mark.parametrize("lens,new", [([5, 1000, 63], [1, 1, 1]), ([100, 0], [90, 70]), ([50] + [7] * 29, [36] + [0] * 8 + [1] * 21), ([3, 62], [1, 2])],
+                         ids=["tokens", "prompts", "prompt-among-tokens", "few"])
 def test_write_with_a_rope(lens, new, layout, dim, d, hq, hkv, fp8):
     g = torch.Generator().manual_seed(dim + hq)
     tokens, pages = sum(new) + 2, 40
+    pages += len(lens)
     table_in, free = tables(lens, pages, 18, np.random.default_rng(6))
     plan = bf1.plan_cache(ints(lens), ints(new), ints(table_in), pages, tokens, stack_of(free, pages), ints([len(free)]))
     k, v = (torch.randn((tokens, hkv, d), generator=g).to(torch.bfloat16).to(DEV) for _ in range(2))

@@ -156,7 +156,7 @@ def test_refusals_of_the_binding():
     rope = bf1.plan_rope(bf1.RopeCfg(64), DEV)
     for bad in (lambda: bf1.rope_fwd(q.float(), k, pos, rope), lambda: bf1.rope_fwd(q, k[:3], pos, rope), lambda: bf1.rope_fwd(q, k, pos[:3], rope),
                 lambda: bf1.rope_fwd(q, k, pos.long(), rope), lambda: bf1.rope_fwd(q, k, pos.cpu(), rope), lambda: bf1.rope_fwd(q, k.cpu(), pos, rope),
-                lambda: bf1.rope_fwd(q, k, pos, rope, out_q=torch.empty_like(k)), lambda: bf1.rope_fwd(q.transpose(1, 2), None, pos, rope),
+                lambda: bf1.rope_fwd(q, k, pos, rope, out_q=torch.empty_like(k)), lambda: bf1.rope_fwd(q, None, pos, rope, out_q=q[:1].expand(4, 2, 64)), lambda: bf1.rope_fwd(q.transpose(1, 2), None, pos, rope),
                 lambda: bf1.rope_fwd(q, k, pos, bf1.plan_rope(bf1.RopeCfg(64), "cpu"))):   # (a table on the host is not read)
         with pytest.raises(AssertionError):
             bad()
