@@ -590,7 +590,8 @@ __global__ void __launch_bounds__(kD8Threads, kMode == kWhole ? 2 : 3) decode8_k
 
 // Adds up the lists that cuts go through: a CTA per list and KV head, parts in list order, run by run.  The parts' weights first, a
 // thread to each, so that their (max, sum) are asked for at once, as the sums are after that (one after the other was 20 us for 55 parts).
-constexpr int kJoinThreads = 256;
+// A CTA has 32 of the columns (four numbers each), so that up to 64 parts are one round of loads.
+constexpr int kJoinThreads = 256, kJoinColumns = 32;
 template <int D>
 __global__ void __launch_bounds__(kJoinThreads) decode8_join_kernel(const Decode8Args a) {
     constexpr int kVec = D / 4;                              // threads to a head's row, 4 columns each
@@ -606,8 +607,8 @@ __global__ void __launch_bounds__(kJoinThreads) decode8_join_kernel(const Decode
     const int j0 = run_of(first), j1 = run_of(last - 1), parts = j1 - j0 + 1;
     if (parts == 1) return;                                  // whole: written already
     auto slot = [&](int j) { return (((size_t)kvh * a.runs + j) * 2 + (j == j0 ? 1 : 0)) * a.group; };
-    const int columns = a.group * kVec, groups = kJoinThreads / columns;
-    const int g = tid / columns, h = tid % columns / kVec, c = tid % kVec;
+    const int columns = min(a.group * kVec, kJoinColumns), groups = kJoinThreads / columns;
+    const int g = tid / columns, column = blockIdx.z * columns + tid % columns, h = column / kVec, c = column % kVec;
     constexpr int kAhead = 8;
     float4 v[kAhead];                                        // this thread's columns of every groups-th part, the first ones asked for now
     auto fetch = [&](int i0) {
@@ -819,7 +820,8 @@ extern "C" int bf1_decode_fwd_fp8(const void* q, const void* k_pages, const void
     const dim3 grid(hkv, mode == kRuns ? a.runs : batch, mode == kParts ? a.nctas : 1);
     BF1_CUDA_CHECK(launch_pdl_cluster(variant.by_mode[mode], grid, dim3(1, 1, grid.z), kD8Threads, smem, (cudaStream_t)stream, tk, tv, a));
     if (mode == kRuns)
-        BF1_CUDA_CHECK(launch_pdl(d == 128 ? decode8_join_kernel<128> : decode8_join_kernel<64>, dim3(hkv, batch), kJoinThreads, 0,
+        BF1_CUDA_CHECK(launch_pdl(d == 128 ? decode8_join_kernel<128> : decode8_join_kernel<64>, dim3(hkv, batch, std::max(1, group * d / 4 / kJoinColumns)),
+                                  kJoinThreads, 0,
                                   (cudaStream_t)stream, a));
     return BF1_OK;
 }

@@ -149,7 +149,8 @@ def test_batches(batch, hq, hkv):
     check(c, q, out, lse)
 
 
-@pytest.mark.parametrize("batch,hq,hkv,d,most", [(90, 4, 2, 64, 2500), (41, 16, 4, 128, 1900), (150, 1, 1, 128, 1700), (1024, 2, 1, 64, 1800), (3, 2, 1, 64, 30000)])
+@pytest.mark.parametrize("batch,hq,hkv,d,most", [(90, 4, 2, 64, 2500), (41, 16, 4, 128, 1900), (150, 1, 1, 128, 1700), (1024, 2, 1, 64, 1800), (3, 2, 1, 64, 30000), (1100, 2, 1, 64, 6000), (9, 16, 4, 64, 29000),
+                                                     (5, 4, 1, 128, 27000)])
 def test_runs_through_lists_of_all_lengths(batch, hq, hkv, d, most):
     """Long lists that fill the GPU: equal runs of the row of all pages, empty lists among them, lists cut once, often and not at all."""
     rng = np.random.default_rng(batch)

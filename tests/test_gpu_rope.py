@@ -114,6 +114,17 @@ def test_padding_rows_stay_and_empty_calls_do_nothing():
     assert oq.shape == (0, 2, 64) and ok.shape == (0, 1, 64)
 
 
+def test_rows_beyond_32_bits():
+    tokens, h, d = (1 << 31) // (64 * 128) + 5, 64, 128
+    q = torch.zeros((tokens, h, d), dtype=torch.bfloat16, device=DEV)
+    q[-5:] = inputs(5, h, 1, d, 13)[0]
+    pos = torch.full((tokens,), -1, dtype=torch.int32, device=DEV)
+    pos[-5:] = torch.arange(5, dtype=torch.int32, device=DEV) + 99
+    rope = bf1.plan_rope(bf1.RopeCfg(d), DEV)
+    want = bf1.rope_fwd(q[-5:], None, pos[-5:], rope)[0]
+    assert torch.equal(bf1.rope_fwd(q, None, pos, rope, out_q=q)[0][-5:], want)
+
+
 def test_gradient_against_differences():
     """d/dx <g, R x> along a direction, from the forward alone: the forward is linear, so a step of any size gives the slope up to
     rounding.  x, y of bf16 values: <g, R x> rounds each product's factor by 2^-8 at most."""
