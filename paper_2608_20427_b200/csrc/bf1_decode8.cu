@@ -254,7 +254,7 @@ struct Merge8 {                          // the four warps' states at the end of
 
 // grid (hkv, runs), (hkv, batch) or (hkv, batch, CTAs of the cluster)
 template <int D, int kHeads, int kMode>
-__global__ void __launch_bounds__(kD8Threads, kMode == kWhole ? 2 : 3) decode8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+__global__ void __launch_bounds__(kD8Threads, kMode != kWhole ? 3 : D == 64 ? 4 : 2) decode8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                                                                 const Decode8Args a) {
     constexpr int kPageBytes = kP8 * D;
     extern __shared__ uint8_t dsmem[];
@@ -446,7 +446,8 @@ __global__ void __launch_bounds__(kD8Threads, kMode == kWhole ? 2 : 3) decode8_k
             if (++stage == a.stages) stage = 0, parity ^= 1;
             return at;
         };
-        for (; kMode != kRuns && x + 1 < end && a.stages > 1; x += 2) {
+        // (a run's ring of three pages of d = 128 would have one on its way while two are taken)
+        for (; (kMode != kRuns || D == 64) && x + 1 < end && a.stages > 1; x += 2) {
             const int p0 = next(), p1 = next();
             const uint32_t kb[2] = {ring + p0 * 2 * kPageBytes, ring + p1 * 2 * kPageBytes};
             const float2 scales[2] = {page_scales[p0], page_scales[p1]};
@@ -786,12 +787,13 @@ extern "C" int bf1_decode_fwd_fp8(const void* q, const void* k_pages, const void
     size_t smem = 1024;
     if (mode == kRuns) {
         // three CTAs of three pages each to an SM: 24 lists of 32K tokens and less, all heads, 130 us; with two CTAs of four to six pages 134 to 137,
-        // three of four 141 (more pages in flight than HBM needs wait for one another)
+        // three of four 141 (more pages in flight than HBM needs wait for one another).  d = 64, where a CTA takes two pages at a step: 40 lists of 20000 tokens,
+        // two heads, 42.6 us with six pages, 44.3 with four or eight, 44.1 with four CTAs, 45.8 page by page
         a.runs = std::max(1, std::min(3 * sms, kD8MaxRuns) / hkv);
         a.stages = d == 128 ? 3 : 6;
         smem += sizeof(int) * (batch + 1);
     } else if (mode == kWhole) {
-        // two CTAs to an SM, or three that hold half as much where there are more lists than that
+        // two CTAs to an SM (with d = 64 four: 512 lists of 12 pages 18.1 -> 13.1 us), which hold half as much where there are more lists than SMs take at once
         a.stages = std::min(most, lists > 2 * sms ? (d == 128 ? 3 : 6) : (d == 128 ? 6 : 8));
     } else {
         // as many CTAs to a list as still let all clusters run at once (a cluster's CTAs share a GPC, so this is less than what the SMs hold)
