@@ -48,15 +48,17 @@ struct Decode8Args {
     int32_t runs;                        // kRuns: per KV head
     int32_t stages, ahead;               // pages in a CTA's ring, and of those asked for at once at the start
     int32_t nctas, share;                // kParts: CTAs to a list, columns (of the heads' G d) that each adds up, a multiple of 32
-    int32_t* bases;                      // workspace: [batch + 1] pages in front of every list
+    int32_t* bases;                      // workspace: [batch + 2] pages in front of every list, runs in use
     float2* part_ml;                     // [hkv][runs][2][group] (max, sum) ...
     float* part_o;                       // [hkv][runs][2][group][d] ... and sum of a cut list's part
 };
 
-// Runs that a row of `pages` pages is cut into: of kD8MinRun pages at least, so that short rows are not all joining (and none is empty).
-__host__ __device__ __forceinline__ int runs_of(int runs, long long pages) {
+// Runs that a row of `pages` pages is cut into: of kD8MinRun pages at least, so that short rows are not all joining (and none is empty), and so that the
+// longest list, of `longest` pages, is cut into no more than four times the root of that: a page more to a run costs what the join of its part would (0.4 us,
+// and 0.03 for each part).
+__device__ __forceinline__ int runs_of(int runs, long long pages, int longest) {
     const long long most = (pages + kD8MinRun - 1) / kD8MinRun;
-    return (int)(most < runs ? most : runs);
+    return (int)fminf((float)min((long long)runs, most), ceilf(4.f * (float)pages * rsqrtf((float)max(longest, 1))));
 }
 
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, int c0, int c1, int c2, uint32_t bar) {
@@ -261,7 +263,7 @@ __global__ void __launch_bounds__(kD8Threads, kMode != kWhole ? 3 : D == 64 ? 4 
     __shared__ uint64_t bars[2 * kD8MaxStages];
     __shared__ float2 page_scales[kD8MaxStages];
     __shared__ Merge8<D, kHeads> st;
-    __shared__ int warp_sums[kD8Threads / 32];
+    __shared__ int warp_sums[kD8Threads / 32], warp_most[kD8Threads / 32];
     __shared__ int abort_flag;
     const uint32_t ring = (smem_u32(dsmem) + 1023) & ~1023u;
     uint8_t* const behind = dsmem + (ring - smem_u32(dsmem)) + (size_t)a.stages * 2 * kPageBytes;
@@ -306,22 +308,26 @@ __global__ void __launch_bounds__(kD8Threads, kMode != kWhole ? 3 : D == 64 ? 4 
         if constexpr (kMode == kParts) cluster_arrive_relaxed();     // (waited for in front of the first store to another CTA)
     } else {
         const int per = (a.batch + kD8Threads - 1) / kD8Threads, lo = min(tid * per, a.batch), hi = min(lo + per, a.batch);
-        int sum = 0;
+        int sum = 0, longest = 0;
         for (int i = lo; i < hi; ++i) {
             const int c = pages_of_list(i, kvh == 0 && blockIdx.y == 0);
             bases[i] = c;
             sum += c;
+            longest = max(longest, c);
         }
         int incl = sum;
+        longest = __reduce_max_sync(0xffffffffu, longest);
 #pragma unroll
         for (int off = 1; off < 32; off <<= 1) {
             const int v = __shfl_up_sync(0xffffffffu, incl, off);
             if (lane >= off) incl += v;
         }
-        if (lane == 31) warp_sums[warp] = incl;
+        if (lane == 31) warp_sums[warp] = incl, warp_most[warp] = longest;
         __syncthreads();
         int at = incl - sum;
         for (int w = 0; w < warp; ++w) at += warp_sums[w];
+#pragma unroll
+        for (int w = 0; w < kD8Threads / 32; ++w) longest = max(longest, warp_most[w]);
         for (int i = lo; i < hi; ++i) {
             const int c = bases[i];
             bases[i] = at;
@@ -330,13 +336,13 @@ __global__ void __launch_bounds__(kD8Threads, kMode != kWhole ? 3 : D == 64 ? 4 
         if (lo < hi && hi == a.batch) bases[a.batch] = at;
         __syncthreads();
         const long long total = bases[a.batch];
-        const int runs = runs_of(a.runs, total);
+        const int runs = runs_of(a.runs, total, longest);
         if ((int)blockIdx.y < runs && total > 0) {
             x0 = (int)(total * blockIdx.y / runs);
             x1 = (int)(total * (blockIdx.y + 1) / runs);
         }
         if (kvh == 0 && blockIdx.y == 0)
-            for (int i = tid; i <= a.batch; i += kD8Threads) a.bases[i] = bases[i];
+            for (int i = tid; i <= a.batch + 1; i += kD8Threads) a.bases[i] = i <= a.batch ? bases[i] : runs;
         if (x0 >= x1) return;
     }
     // the list that page x belongs to
@@ -603,7 +609,7 @@ __global__ void __launch_bounds__(kJoinThreads) decode8_join_kernel(const Decode
     const int kvh = blockIdx.x, s = blockIdx.y, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const long long total = a.bases[a.batch], first = a.bases[s], last = a.bases[s + 1];
     if (first == last) return;
-    const long long runs = runs_of(a.runs, total);
+    const long long runs = a.bases[a.batch + 1];
     auto run_of = [&](long long x) { return (int)(((x + 1) * runs - 1) / total); };   // the last run that begins at or in front of page x
     const int j0 = run_of(first), j1 = run_of(last - 1), parts = j1 - j0 + 1;
     if (parts == 1) return;                                  // whole: written already
@@ -713,7 +719,7 @@ extern "C" int64_t bf1_decode_fp8_workspace_bytes(int32_t batch, int32_t hq, int
     if (batch < 0 || hq <= 0 || hkv <= 0 || hq % hkv != 0 || max_degree <= 0 || d <= 0) return -1;
     if (batch > kD8MaxScan) return 16;
     const size_t parts = (size_t)std::max(1, kD8MaxRuns / hkv) * hkv * 2 * (hq / hkv);
-    return (int64_t)(up16(sizeof(int32_t) * ((size_t)batch + 1)) + parts * (sizeof(float2) + sizeof(float) * d));
+    return (int64_t)(up16(sizeof(int32_t) * ((size_t)batch + 2)) + parts * (sizeof(float2) + sizeof(float) * d));
 }
 
 extern "C" int bf1_decode_fwd_fp8(const void* q, const void* k_pages, const void* v_pages, const float* k_scales, const float* v_scales,
@@ -771,34 +777,25 @@ extern "C" int bf1_decode_fwd_fp8(const void* q, const void* k_pages, const void
     const int64_t lists = (int64_t)batch * hkv;
     const int most = plan->max_degree;
     auto ceil_div = [](int64_t x, int64_t y) { return (int)((x + y - 1) / y); };
-    // Which way, by what the host knows: the number of lists and the longest that there may be.  Over 796 shapes (1 to 1120 lists of up to 1
+    // Which way, by what the host knows: the number of lists and the longest that there may be.  Over 784 shapes (1 to 1120 lists of up to 1
     // to 400 pages, d = 64 and 128, two and four heads; lists alike, from short to the longest evenly, and mostly short ones; on pages that no cache
-    // holds) this takes 2.2 % longer on average than the best of the three, mostly where one list is far longer than the others.  us in
-    // runs / whole / in parts (16 query / 8 KV heads, d = 128):
+    // holds) this takes 1.2 % longer on average than the best of the three.  us in runs / whole / in parts (16 query / 8 KV heads, d = 128):
     //   up to two pages a cluster never pays: one sequence of 1 / 2 pages 2.9 / 3.3 whole, 4.1 / 3.9 in parts;
     //   lists for every SM: 32 sequences of 12 pages 19.5 / 12.9 / 14.6, 140 of 4 27 / 25 / 26, 32 alike of 48 40 / 34 / 38, 64 of 48 71 / 87 / 83,
     //     64 of up to 48, mostly short, 26 / 39 / 30;
-    //   fewer: one sequence of 12 / 48 / 200 / 400 pages 9.2 / 7.3 / 4.4, 11.7 / 23 / 7.5, 15.4 / 84 / 13.3, 19.7 / 164 / 20.0, eight of 48 / 200
-    //     18.6 / 23 / 14.3, 41 / 85 / 38, of up to 200, mostly short, 20.9 / 83 / 21.7.
+    //   fewer, in parts of up to 20 pages: one sequence of 12 / 48 / 200 / 400 pages 9.2 / 7.3 / 4.4, 11.7 / 23 / 7.5, 15.4 / 84 / 13.3, 19.7 / 164 / 20.0,
+    //     eight of 48 / 200 18.6 / 23 / 14.3, 41 / 85 / 38, of up to 200, mostly short, 20.9 / 83 / 21.7.  Longer parts lose little where lists are alike and
+    //     all where one is alone: 16000 tokens beside eleven sequences of 958 17 in runs, 29 in parts of 52 pages (4 KV heads).
     int mode = kRuns;
     if (batch > kD8MaxScan || most <= 2 || (lists >= sms && most <= 24)) mode = kWhole;
-    else if (lists < sms && most <= 400 && most * lists <= 14000) mode = kParts;
+    else if (lists < sms && most <= 20 * kD8MaxCtas) mode = kParts;
     a.runs = a.nctas = a.share = 0;
     size_t smem = 1024;
-    if (mode == kRuns) {
-        // three CTAs of three pages each to an SM: 24 lists of 32K tokens and less, all heads, 130 us; with two CTAs of four to six pages 134 to 137,
-        // three of four 141 (more pages in flight than HBM needs wait for one another).  d = 64, where a CTA takes two pages at a step: 40 lists of 20000 tokens,
-        // two heads, 42.6 us with six pages, 44.3 with four or eight, 44.1 with four CTAs, 45.8 page by page
-        a.runs = std::max(1, std::min(3 * sms, kD8MaxRuns) / hkv);
-        a.stages = d == 128 ? 3 : 6;
-        smem += sizeof(int) * (batch + 1);
-    } else if (mode == kWhole) {
-        // two CTAs to an SM (with d = 64 four: 512 lists of 12 pages 18.1 -> 13.1 us), which hold half as much where there are more lists than SMs take at once
-        a.stages = std::min(most, lists > 2 * sms ? (d == 128 ? 3 : 6) : (d == 128 ? 6 : 8));
-    } else {
+    if (mode == kParts) {
         // as many CTAs to a list as still let all clusters run at once (a cluster's CTAs share a GPC, so this is less than what the SMs hold)
-        for (int ctas = (int)std::min<int64_t>({kD8MaxCtas, most, (3 * (int64_t)sms + lists - 1) / lists}); ctas >= 1; --ctas) {
+        for (int ctas = (int)std::min<int64_t>({kD8MaxCtas, most, (3 * (int64_t)sms + lists - 1) / lists}); mode == kParts; --ctas) {
             const int pages = ceil_div(most, ctas);      // of a CTA, at most
+            if (pages > 20) mode = kRuns;
             ctas = ceil_div(most, pages);                // (no more than that takes)
             a.nctas = ctas;
             a.share = ceil_div(heads * d / 32, ctas) * 32;
@@ -810,11 +807,23 @@ extern "C" int bf1_decode_fwd_fp8(const void* q, const void* k_pages, const void
             if (lists <= fit) break;
         }
     }
+    if (mode == kRuns) {
+        // three CTAs of three pages each to an SM: 24 lists of 32K tokens and less, all heads, 130 us; with two CTAs of four to six pages 134 to 137,
+        // three of four 141 (more pages in flight than HBM needs wait for one another).  d = 64, where a CTA takes two pages at a step: 40 lists of 20000 tokens,
+        // two heads, 42.6 us with six pages, 44.3 with four or eight, 44.1 with four CTAs, 45.8 page by page
+        a.nctas = a.share = 0;
+        smem = 1024 + sizeof(int) * (batch + 1);
+        a.runs = std::max(1, std::min(3 * sms, kD8MaxRuns) / hkv);
+        a.stages = d == 128 ? 3 : 6;
+    } else if (mode == kWhole) {
+        // two CTAs to an SM (with d = 64 four: 512 lists of 12 pages 18.1 -> 13.1 us), which hold half as much where there are more lists than SMs take at once
+        a.stages = std::min(most, lists > 2 * sms ? (d == 128 ? 3 : 6) : (d == 128 ? 6 : 8));
+    }
     // not the whole ring at the start: the first page would land later (32 sequences of 12 pages 12.4 us with all six at once, 12.2 with three)
     a.ahead = mode == kRuns ? 2 : 3;
     smem += (size_t)a.stages * page_bytes;
     a.bases = (int32_t*)workspace;
-    a.part_ml = (float2*)((uint8_t*)workspace + up16(sizeof(int32_t) * ((size_t)batch + 1)));
+    a.part_ml = (float2*)((uint8_t*)workspace + up16(sizeof(int32_t) * ((size_t)batch + 2)));
     a.part_o = (float*)(a.part_ml + (size_t)hkv * a.runs * 2 * group);
     CUtensorMap tk, tv;
     if (int rc = make_page_map(&tk, k_pages, num_pages, hkv, d)) return rc;
