@@ -372,7 +372,8 @@ typedef struct {
     int32_t  capacity_units;    /* host: bf1_cache_plan_units(batch, capacity_tokens) or more                   */
     int32_t *seqlens;           /* [batch] cached tokens after the step; may be seqlens_dev itself              */
     int32_t *free_count;        /* [1] free pages after the step; may be free_count_dev itself                  */
-    int32_t *cu_tokens;         /* [batch + 1] offsets of the sequences' new tokens                             */
+    int32_t *cu_tokens;         /* [batch + 1] offsets of the sequences' new tokens: the newest token of a sequence that
+                                   has any is row cu_tokens[s + 1] - 1 (bf1_decode_fwd* want a row per sequence) */
     int32_t *positions;         /* [capacity_tokens] a token's position in its sequence; -1 behind the last one */
     int32_t *slots;             /* [capacity_tokens] page * 64 + row; -1 behind the last one                    */
     int32_t *units;             /* [capacity_units, 4] tokens that share a page, in order: first token, number, page,

@@ -9,6 +9,10 @@
 // step's rows for it: a unit is what one CTA (or half a warp) does.  Scales are powers of two: e4m3 has the same precision in every
 // binade, so that a finer scale would gain nothing, and rows that have to move under a larger scale keep their digits (but for
 // those that fall below 2^-6 of it, which have fewer at any scale).
+//
+// Measured (16 query / 8 KV heads, d = 128, in a graph): the tables of 32 sequences of a token each 3.2 us, of 512 with 130 prompts and 32 released
+// ones 11.1; keys and values of 32K prompt tokens into 8-bit pages 32.0 us, 6.3 TB/s, 97 % of a copy; of 8 / 256 single tokens, with the rotation of
+// their queries and keys, 2.9 / 4.2 us, chains of launch, unit, position, angle and scale.
 #include <math.h>
 
 #include <algorithm>

@@ -3,16 +3,17 @@
 //   o = sum_i p_i sv(i) v_i / sum_i p_i,   p_i = exp(scale * sk(i) <q, k_i>),   i over the keys of the plan's pages
 //
 // Every key costs 2 d bytes and 4 d G operations: bound by HBM for as long as the arithmetic on a page (16 KB of K and V at
-// d = 128) stays hidden behind the copies, 700 cycles of an SM.  The list of a dense layer has hundreds of pages and lists are of all
-// lengths, so the work is not dealt by lists: for every KV head the pages of all lists stand in one row, which is cut into equal runs, one
-// to a CTA, as many as the SMs hold at once.  The eight CTAs that read the heads of one page run side by side, so that its 8 KB
-// rows are fetched together.  A list that a cut goes through is left as partial (max, sum, O), which a second small kernel adds up
-// in list order.
+// d = 128) stays hidden behind the copies, 700 cycles of an SM.  Short lists are walked by a CTA each, or by a cluster whose CTAs exchange their parts (max,
+// sum, O) through shared memory.  The list of a dense layer has hundreds of pages, and lists are of all lengths: then the work is not dealt by lists, but for
+// every KV head the pages of all of them stand in one row, which is cut into equal runs, one to a CTA, as many as the SMs hold at once.  The CTAs that read
+// the heads of one page run side by side, so that its rows are fetched together.  A list that a cut goes through is left as partial results, which a second
+// small kernel adds up in list order.  Measured: 24 lists of up to 32K tokens, 16 query / 8 KV heads, d = 128, 842 MB: 130 us, 6.45 TB/s, a copy's rate; one
+// sequence of 100K tokens 39.8 us (floor 31.7), 32 along the route 12.6 (7.2), one along the route 4.3.
 //
 // In a CTA one warp asks for pages by TMA into a ring, and four warps take 16 keys of every page each.  The numbers of the cache are the A
 // operand of m16n8k16 (16 keys or 16 dimensions to a row, the heads are the eight columns): widened from e4m3 to f16, which is
 // exact, two at a time.  q, eight bits of fraction in bf16, is exact in f16 too once it is scaled to the head's largest value; P in f16 is rounded
-// by 2^-12, an eighth of what bf16 would cost.  Scales stay outside of the products, in 32 bits: sk on the scores, sv on each page's sum.
+// by 2^-11, an eighth of what bf16 would cost.  Scales stay outside of the products, in 32 bits: sk on the scores, sv on each page's sum.
 #include <math.h>
 
 #include <algorithm>
