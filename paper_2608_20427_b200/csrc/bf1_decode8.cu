@@ -257,7 +257,7 @@ struct Merge8 {                          // the four warps' states at the end of
 
 // grid (hkv, runs), (hkv, batch) or (hkv, batch, CTAs of the cluster)
 template <int D, int kHeads, int kMode>
-__global__ void __launch_bounds__(kD8Threads, kMode != kWhole ? 3 : D == 64 ? 4 : 2) decode8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+__global__ void __launch_bounds__(kD8Threads, kMode == kWhole && D == 64 ? 4 : 3) decode8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                                                                 const Decode8Args a) {
     constexpr int kPageBytes = kP8 * D;
     extern __shared__ uint8_t dsmem[];
@@ -817,8 +817,9 @@ extern "C" int bf1_decode_fwd_fp8(const void* q, const void* k_pages, const void
         a.runs = std::max(1, std::min(3 * sms, kD8MaxRuns) / hkv);
         a.stages = d == 128 ? 3 : 6;
     } else if (mode == kWhole) {
-        // two CTAs to an SM (with d = 64 four: 512 lists of 12 pages 18.1 -> 13.1 us), which hold half as much where there are more lists than SMs take at once
-        a.stages = std::min(most, lists > 2 * sms ? (d == 128 ? 3 : 6) : (d == 128 ? 6 : 8));
+        // Two CTAs to an SM with a ring of six pages, or, where there are more lists than that, three with four (d = 64: four): 320 / 384 / 512 / 1120 lists of 11 pages,
+        // d = 128, 14.5 / 15.6 / 24.2 / 40.3 us, 22.1 / 23.6 / 25.4 / 48.4 with two CTAs in as many waves as that takes; 512 of 12, d = 64, 18.1 and 13.1
+        a.stages = std::min(most, lists > 2 * sms ? (d == 128 ? 4 : 6) : (d == 128 ? 6 : 8));
     }
     // not the whole ring at the start: the first page would land later (32 sequences of 12 pages 12.4 us with all six at once, 12.2 with three)
     a.ahead = mode == kRuns ? 2 : 3;
