@@ -161,6 +161,10 @@ __global__ void __launch_bounds__(kTableThreads, 1) plan_cache_kernel(const Tabl
         __syncthreads();
     }
     if (gtid == 0) *p.free_count = top - at.y;
+    // Every look-up and store below keeps to its array for whatever numbers the scan has made of lengths that have changed since they were added up.
+    auto pop = [&](int i) { return (unsigned)i < (unsigned)top ? a.free_pages[top - 1 - i] : -1; };     // the i-th page taken
+    auto row_of = [&](int s) { return a.table + (size_t)s * a.max_pages; };
+    auto in_row = [&](int i) { return (unsigned)i < (unsigned)a.max_pages; };
     // ---- lengths after the step; pages put back ------------------------------------------------------------------------------------
     // All warps share the sequences, and the units below, a few to each: what is done for one after the other waits for memory each time
     // (32 to a warp, and most warps idle: 512 sequences, 130 of them prompts, 18.1 us)
@@ -181,12 +185,12 @@ __global__ void __launch_bounds__(kTableThreads, 1) plan_cache_kernel(const Tabl
         const int held = pages_of(n), want = stack && m > 0 ? pages_of(n + m) - held : 0;
         if (at.w == 0) {
             unsigned grown = __ballot_sync(0xffffffffu, want > 1);
-            if (want == 1) a.table[(size_t)s * a.max_pages + held] = a.free_pages[top - 1 - to];
+            if (want == 1 && in_row(held)) row_of(s)[held] = pop(to);
             while (grown) {
                 const int l = __ffs(grown) - 1;
                 grown &= grown - 1;
                 const int count = __shfl_sync(0xffffffffu, want, l), h = __shfl_sync(0xffffffffu, held, l), f = __shfl_sync(0xffffffffu, to, l);
-                for (int i = lane; i < count; i += 32) a.table[(size_t)(s0 + l) * a.max_pages + h + i] = a.free_pages[top - 1 - (f + i)];
+                for (int i = lane; i < count && in_row(h + i); i += 32) row_of(s0 + l)[h + i] = pop(f + i);
             }
         } else {
             unsigned gone = __ballot_sync(0xffffffffu, m < 0);
@@ -194,7 +198,7 @@ __global__ void __launch_bounds__(kTableThreads, 1) plan_cache_kernel(const Tabl
                 const int l = __ffs(gone) - 1;
                 gone &= gone - 1;
                 const int count = __shfl_sync(0xffffffffu, held, l), first = had + __shfl_sync(0xffffffffu, to, l);
-                for (int i = lane; i < count; i += 32) a.free_pages[first + i] = a.table[(size_t)(s0 + l) * a.max_pages + i];
+                for (int i = lane; i < count && in_row(i) && (unsigned)(first + i) < (unsigned)a.num_pages; i += 32) a.free_pages[first + i] = row_of(s0 + l)[i];
             }
         }
     }
@@ -221,7 +225,7 @@ __global__ void __launch_bounds__(kTableThreads, 1) plan_cache_kernel(const Tabl
                 const int l = __ffs(grown) - 1;
                 grown &= grown - 1;
                 const int count = __shfl_sync(0xffffffffu, want, l), h = __shfl_sync(0xffffffffu, held, l), f = __shfl_sync(0xffffffffu, first, l);
-                for (int i = lane; i < count; i += 32) a.table[(size_t)(s0 + l) * a.max_pages + h + i] = a.free_pages[top - 1 - (f + i)];
+                for (int i = lane; i < count && in_row(h + i); i += 32) row_of(s0 + l)[h + i] = pop(f + i);
             }
         }
     }
@@ -243,7 +247,8 @@ __global__ void __launch_bounds__(kTableThreads, 1) plan_cache_kernel(const Tabl
             t = st.x + (pos - st.w);
             const int row = pos % kCachePage;
             count = min(kCachePage - row, end - t);
-            int page = stack && lp >= held ? a.free_pages[top - 1 - (st.y + lp - held)] : a.table[(size_t)lo * a.max_pages + lp];
+            int page = stack && lp >= held ? pop(st.y + lp - held) : in_row(lp) ? row_of(lo)[lp] : -1;
+            count = t < 0 ? 0 : min(count, p.capacity_tokens - t);
             if (page < 0 || page >= a.num_pages) {
                 atomicOr(p.status, BF1_DEV_BAD_ROUTE);
                 page = -1;
@@ -251,8 +256,10 @@ __global__ void __launch_bounds__(kTableThreads, 1) plan_cache_kernel(const Tabl
                 slot = page * kCachePage + row;
             }
             if (u < p.capacity_units) reinterpret_cast<int4*>(p.units)[u] = make_int4(t, count, page, row);
-            p.positions[t] = pos;                         // (single tokens, side by side in a step of them)
-            p.slots[t] = slot;
+            if (count > 0) {
+                p.positions[t] = pos;                     // (single tokens, side by side in a step of them)
+                p.slots[t] = slot;
+            }
         }
         unsigned more = __ballot_sync(0xffffffffu, count > 1);
         while (more) {

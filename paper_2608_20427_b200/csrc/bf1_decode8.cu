@@ -265,7 +265,7 @@ __global__ void __launch_bounds__(kD8Threads, kMode == kWhole && D == 64 ? 4 : 3
     __shared__ float2 page_scales[kD8MaxStages];
     __shared__ Merge8<D, kHeads> st;
     __shared__ int warp_sums[kD8Threads / 32], warp_most[kD8Threads / 32];
-    __shared__ int abort_flag;
+    __shared__ int abort_flag, list_count;
     const uint32_t ring = (smem_u32(dsmem) + 1023) & ~1023u;
     uint8_t* const behind = dsmem + (ring - smem_u32(dsmem)) + (size_t)a.stages * 2 * kPageBytes;
     int* const bases = reinterpret_cast<int*>(behind);                 // kRuns
@@ -283,7 +283,7 @@ __global__ void __launch_bounds__(kD8Threads, kMode == kWhole && D == 64 ? 4 : 3
         tma_prefetch_desc(&tm_v);
     }
     pdl_wait();
-    const bool reports = kvh == 0 && tid == 0 && (kMode == kParts ? blockIdx.z == 0 : true);
+    const bool reports = kvh == 0 && blockIdx.z == 0;
     auto pages_of_list = [&](int s, bool report) {
         const int n = a.seqlens[s];
         const int c = max(min(a.count[s], a.max_degree), 0);
@@ -301,11 +301,13 @@ __global__ void __launch_bounds__(kD8Threads, kMode == kWhole && D == 64 ? 4 : 3
 #pragma unroll
             for (int i = 0; i < 2; ++i)
                 if (lane + 32 * i < a.max_degree) held[i] = a.page[(size_t)s * a.max_degree + lane + 32 * i];
-        count = pages_of_list(s, reports);
+        // read once, since threads that disagreed would not meet at the barriers, and not by the thread that sets these up
+        if (tid == 32) list_count = pages_of_list(s, reports);
+        __syncthreads();                                             // the barriers are there
+        count = list_count;
         x0 = kMode == kParts ? blockIdx.z * count / a.nctas : 0;
         x1 = kMode == kParts ? (blockIdx.z + 1) * count / a.nctas : count;
         if (kMode == kWhole && count == 0) return;
-        __syncthreads();                                             // the barriers are there
         if constexpr (kMode == kParts) cluster_arrive_relaxed();     // (waited for in front of the first store to another CTA)
     } else {
         const int per = (a.batch + kD8Threads - 1) / kD8Threads, lo = min(tid * per, a.batch), hi = min(lo + per, a.batch);
