@@ -164,6 +164,15 @@ def test_runs_through_lists_of_all_lengths(batch, hq, hkv, d, most):
     check(c, q, out, lse)
 
 
+@pytest.mark.parametrize("hkv,group,lens", [(64, 1, [5000, 64, 0, 1700]), (700, 2, [100, 65]), (700, 1, [1800, 3]), (36, 4, [130, 7])])
+def test_many_heads(hkv, group, lens):
+    """More KV heads than a run to each, lists for every SM from few sequences."""
+    c = Cache(lens, hkv, 64, True, seed=hkv)
+    q = queries(len(lens), hkv * group, 64, 15)
+    out, lse, _ = run(c, q)
+    check(c, q, out, lse)
+
+
 def test_scales_of_all_sizes_and_a_given_softmax_scale():
     """A page's weights are rounded against the softmax's maximum alone: a page of tiny values beside huge ones loses nothing of its own."""
     c = Cache([1000, 64, 130], 2, 64, True, seed=4, exponents=(-9, -8))
