@@ -228,7 +228,8 @@ int bf1_decode_fwd(const void *q, const void *k_pages, const void *v_pages, int3
 /* The same step over a cache in 8 bits: k_pages / v_pages hold e4m3 numbers, [num_pages, 64, hkv, d], each page and KV head under
  * an fp32 scale, [num_pages, hkv] (value = number * scale; bf1_cache_write makes powers of two, any are taken).  Half the bytes
  * of the bf16 cache are read; scores, softmax and sums are in 32 bits, the numbers themselves enter the products exactly and P
- * rounded to 11 bits.  Lists may be of any length (the plan's max_degree is not limited to 64), so that layers which stay dense
+ * rounded to 11 bits, or to 2^-39 of the largest among the 16 keys of a page that are taken together where it is below 2^-29
+ * of that (v_scales below 2^-111 lose digits besides).  Lists may be of any length (the plan's max_degree is not limited to 64), so that layers which stay dense
  * are served too: plan them with the route {64, local_blocks >= max_pages_per_seq, 0, 0}.
  *   workspace    device, 16-byte aligned, bf1_decode_fp8_workspace_bytes() bytes, whatever they hold.  It carries a call's partial
  *                results: calls that may overlap on the GPU need one each

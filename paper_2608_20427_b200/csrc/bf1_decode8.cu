@@ -13,7 +13,10 @@
 // In a CTA one warp asks for pages by TMA into a ring, and four warps take 16 keys of every page each.  The numbers of the cache are the A
 // operand of m16n8k16 (16 keys or 16 dimensions to a row, the heads are the eight columns): widened from e4m3 to f16, which is
 // exact, two at a time.  q, eight bits of fraction in bf16, is exact in f16 too once it is scaled to the head's largest value; P in f16 is rounded
-// by 2^-11, an eighth of what bf16 would cost.  Scales stay outside of the products, in 32 bits: sk on the scores, sv on each page's sum.
+// by 2^-11, an eighth of what bf16 would cost.  So that this holds for small weights too, P is made against the largest of the sixteen keys (not of the list) and
+// enters times 2^15: f16 has all its digits down to 2^-29 of that one, and steps of 2^-39 of it below.  (Against the list's largest and times 1, a key 17 nats
+// above the others took all weight from those that its warp saw: with a value of zero it left nothing but rounding.)  Scales stay outside of the
+// products, in 32 bits: sk on the scores, sv on each page's sum, together with the weight of the sixteen keys' largest in the list.
 #include <math.h>
 
 #include <algorithm>
@@ -33,6 +36,7 @@ constexpr int kD8MaxRuns = 640;          // runs at most, which is what the work
 constexpr int kD8MinRun = 4;             // pages of a run at least
 constexpr int kD8MaxCtas = 16;           // to a cluster
 constexpr int kD8Held = 64;              // pages of a list that the copying warp holds at once
+constexpr float kPUp = 32768.f;          // P enters the products times 2^15, so that f16 has eleven digits of it down to 2^-29
 
 // How the lists are dealt: kRuns as above; kWhole a CTA per list; kParts a cluster per list, each CTA an even part of it.
 enum { kRuns, kWhole, kParts };
@@ -155,7 +159,7 @@ struct WarpState {
 };
 
 // Keys key0 .. key0 + 15 of kPages pages in shared memory (K, and V behind it), of which the first `valid` of the last page count.
-// Two pages at a time: their chains of dependent products run side by side, and one look for the maximum serves both.
+// Two pages at a time: their chains of dependent products run side by side.
 template <int D, int kPages>
 __device__ __forceinline__ void page_step(WarpState<D>& w, const uint32_t (&kb)[kPages], int key0, int valid, const uint32_t (&qb)[D / 16][2],
                                           const float (&f)[2], const float2 (&scales)[kPages]) {
@@ -188,33 +192,42 @@ __device__ __forceinline__ void page_step(WarpState<D>& w, const uint32_t (&kb)[
 #pragma unroll
         for (int p = 0; p < kPages; ++p) ldsm4_trans(kb[p] + kP8 * D + page_chunk<D>(row, c + odd), v[p][c / 2]);
     // keys gid (0, 1) and gid + 8 (2, 3) of heads 2 tig and 2 tig + 1
-    float mx[2] = {-INFINITY, -INFINITY}, al[2], base[2];
+    float mx[kPages][2], al[2], base[2], by[kPages][2];
 #pragma unroll
     for (int p = 0; p < kPages; ++p)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const float by = f[h] * scales[p].x;
+            const float to = f[h] * scales[p].x;
             const int there = p == kPages - 1 ? valid : kP8;
-            sc[p][h] = key0 + gid < there ? (sc[p][h] + sd[p][h]) * by : -INFINITY;
-            sc[p][2 + h] = key0 + gid + 8 < there ? (sc[p][2 + h] + sd[p][2 + h]) * by : -INFINITY;
-            mx[h] = fmaxf(mx[h], fmaxf(sc[p][h], sc[p][2 + h]));
+            sc[p][h] = key0 + gid < there ? (sc[p][h] + sd[p][h]) * to : -INFINITY;
+            sc[p][2 + h] = key0 + gid + 8 < there ? (sc[p][2 + h] + sd[p][2 + h]) * to : -INFINITY;
+            mx[p][h] = fmaxf(sc[p][h], sc[p][2 + h]);
         }
 #pragma unroll
     for (int off = 4; off < 32; off <<= 1)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], off));
+        for (int p = 0; p < kPages; ++p)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) mx[p][h] = fmaxf(mx[p][h], __shfl_xor_sync(0xffffffffu, mx[p][h], off));
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const float m = fmaxf(w.m[h], mx[h]);
+        float m = w.m[h];
+#pragma unroll
+        for (int p = 0; p < kPages; ++p) m = fmaxf(m, mx[p][h]);
         base[h] = m == -INFINITY ? 0.f : m;                  // (scores of minus infinity alone)
         al[h] = ex2_approx(w.m[h] - base[h]);
         w.m[h] = m;
         w.l[h] *= al[h];
 #pragma unroll
-        for (int p = 0; p < kPages; ++p) {
-            sc[p][h] = ex2_approx(sc[p][h] - base[h]);
-            sc[p][2 + h] = ex2_approx(sc[p][2 + h] - base[h]);
-            w.l[h] += sc[p][h] + sc[p][2 + h];
+        for (int p = 0; p < kPages; ++p) {                   // weights against the sixteen keys' own largest, which `by` brings to the list's
+            const float own = mx[p][h] == -INFINITY ? 0.f : mx[p][h];
+            sc[p][h] = ex2_approx(sc[p][h] - own);
+            sc[p][2 + h] = ex2_approx(sc[p][2 + h] - own);
+            by[p][h] = ex2_approx(mx[p][h] - base[h]);       // 0 where no key counts
+            w.l[h] = fmaf(by[p][h], sc[p][h] + sc[p][2 + h], w.l[h]);
+            sc[p][h] *= kPUp;
+            sc[p][2 + h] *= kPUp;
+            by[p][h] *= scales[p].y * (1.f / kPUp);
         }
     }
     const bool rescale = __any_sync(0xffffffffu, al[0] != 1.f || al[1] != 1.f);
@@ -238,13 +251,13 @@ __device__ __forceinline__ void page_step(WarpState<D>& w, const uint32_t (&kb)[
             uint32_t r[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) r[i] = __byte_perm(v[p][c / 2][i], 0, 0x3120);     // (two keys of one dimension side by side)
-            const uint64_t by = pack2(scales[p].y, scales[p].y);
+            const uint64_t by2 = pack2(by[p][0], by[p][1]);
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 float pa[4] = {0.f, 0.f, 0.f, 0.f};
                 mma_f16(pa, widen_lo(r[2 * u]), widen_hi(r[2 * u]), widen_lo(r[2 * u + 1]), widen_hi(r[2 * u + 1]), b[p][0], b[p][1]);
 #pragma unroll
-                for (int i = 0; i < 2; ++i) w.acc[c + u][i] = fma2(by, pack2(pa[2 * i], pa[2 * i + 1]), w.acc[c + u][i]);
+                for (int i = 0; i < 2; ++i) w.acc[c + u][i] = fma2(by2, pack2(pa[2 * i], pa[2 * i + 1]), w.acc[c + u][i]);
             }
         }
     }

@@ -390,3 +390,62 @@ def test_a_serving_loop(dense):
     new.copy_(torch.tensor([-1, 1, 1], dtype=torch.int32))
     graph.replay()
     assert lens[0].item() == 0 and count.item() >= before + held - 2 and torch.equal(out[0], was) and pages_plan.count[0].item() == 0
+
+
+def check_beside(c, q, out, lse):
+    """As `check`, with what is small held to its own size: a weight's rounding to f16 is 2^-11 of it, but for those below 2^-29 of the
+    largest among the sixteen keys of a page that a warp takes together, which are off by half of 2^-39 of that one."""
+    q64, kp, vp, ks, vs = (t.double().cpu().numpy() for t in (q, c.kp, c.vp, c.ks, c.vs))
+    batch, hq, d = q.shape
+    want, want_lse = C.decode(q64, kp, vp, ks, vs, c.lists, c.lens)
+    got, got_lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    for s, (x, n) in enumerate(zip(c.lists, c.lens)):
+        keys = (len(x) - 1) * 64 + (n - 1) % 64 + 1
+        for h in range(hq):
+            j = h // (hq // kp.shape[2])
+            k = (kp[x, :, j] * ks[x, j][:, None, None]).reshape(-1, d)[:keys]
+            v = np.abs(vp[x, :, j] * vs[x, j][:, None, None]).reshape(-1, d)[:keys]
+            score = k @ q64[s, h] / math.sqrt(d)
+            off = d * 2.0 ** -24 * (np.abs(k) @ np.abs(q64[s, h])).max() / math.sqrt(d) + 2.0 ** -21 * (np.abs(score).max() + 1)
+            w = np.exp(score - want_lse[h, s])
+            limit = 2.0 ** -8 * np.abs(want[s, h]) + (2.0 ** -11 + 2 * off) * 1.01 * (w @ v)
+            for i in range(0, keys, 16):
+                limit = limit + 2.0 ** -40 * w[i:i + 16].max() * v[i:i + 16].sum(0)
+            assert (np.abs(got[s, h] - want[s, h]) <= limit).all(), (s, h, (np.abs(got[s, h] - want[s, h]) / limit).max())
+            assert abs(got_lse[h, s] - want_lse[h, s]) <= off + 2.0 ** -21 * (1 + abs(want_lse[h, s])), (s, h)
+
+
+@pytest.mark.parametrize("lens,hq,hkv,d,dense", [([30000], 2, 1, 128, True), ([1536, 700, 65, 40], 16, 8, 128, True), ([32768], 4, 1, 64, False), ([500] * 160, 1, 1, 64, True),
+                                                 ([22000, 100, 3000], 8, 2, 64, True)], ids=["runs", "parts", "route", "whole", "runs-64"])
+@pytest.mark.parametrize("nats", [12.0, 17.0, 18.5, 20.0, 30.0])
+def test_a_sink_takes_nothing_from_the_others(nats, lens, hq, hkv, d, dense):
+    """One key far above all others and with a value of zero: the result is the others', with their digits, however small their weights."""
+    c = Cache(lens, hkv, d, dense, seed=16)
+    c.kp = (c.kp.float() / 16).to(E4M3)
+    c.ks.fill_(2.0 ** -5)
+    q = torch.ones((len(lens), hq, d), dtype=torch.bfloat16) * (torch.randint(0, 2, (len(lens), hq, d), generator=torch.Generator().manual_seed(17)) * 2 - 1)
+    q[:, :] = q[:, :1]                                              # one sign pattern for the heads, so that one key is everyone's sink
+    for s, x in enumerate(c.lists):
+        at = (7 * s) % min(lens[s], 64)                             # in the first page of the list
+        c.kp[x[0], at] = (q[s, 0].float() * (nats / math.sqrt(d)) * 32).to(E4M3)
+        c.vp[x[0], at] = 0
+    out, lse, _ = run(c, q)
+    check_beside(c, q, out, lse)
+
+
+@pytest.mark.parametrize("lens,hq,hkv,d", [([256] * 3, 2, 1, 128), ([256] * 160, 2, 1, 128), ([25600], 2, 1, 128), ([25600], 2, 1, 64)], ids=["parts", "whole", "runs", "runs-64"])
+def test_pages_of_small_weights_and_large_values(lens, hq, hkv, d):
+    """Every other page has scores 18 nats below its neighbours' and values 2^40 times theirs: it is what the result is made of."""
+    for odd in (0, 1):
+        c = Cache(lens, hkv, d, True, seed=18)
+        c.kp = (c.kp.float() / 16).to(E4M3)
+        c.ks.fill_(2.0 ** -5)
+        q = torch.ones((len(lens), hq, d), dtype=torch.bfloat16)
+        c.vs.fill_(2.0 ** -7)
+        for x in c.lists:
+            for b, p in enumerate(x):
+                if b % 2 == odd:
+                    c.kp[p] = (c.kp[p].float() + 18.0 / math.sqrt(d) * 32).to(E4M3)
+                    c.vs[p] = 2.0 ** -47
+        out, lse, _ = run(c, q)
+        check_beside(c, q, out, lse)
