@@ -239,6 +239,15 @@ int bf1_decode_fwd_fp8(const void *q, const void *k_pages, const void *v_pages, 
                        int32_t num_pages, const int32_t *seqlens_dev, int32_t batch, int32_t hq, int32_t hkv, int32_t d,
                        float softmax_scale, const bf1_decode_plan *plan /* host */, void *workspace, void *o, float *lse,
                        void *stream);
+/* The same on a step's packed rows, as bf1_plan_cache numbers them and bf1_cache_write takes them: q and o are [tokens, hq, d], lse is
+ * [hq, tokens], and the newest token of sequence s is row cu_tokens[s + 1] - 1.  A sequence without a token in the step
+ * (cu_tokens[s] = cu_tokens[s + 1]: idle, released, or the step was refused) is passed over; the rows of its other tokens and those
+ * behind the last one are not read and not written.  Offsets outside [0, tokens] set BF1_DEV_BAD_ROUTE and the sequence is passed over.
+ *   cu_tokens_dev  [batch + 1] device */
+int bf1_decode_fwd_fp8_packed(const void *q, int32_t tokens, const int32_t *cu_tokens_dev, const void *k_pages, const void *v_pages,
+                              const float *k_scales, const float *v_scales, int32_t num_pages, const int32_t *seqlens_dev,
+                              int32_t batch, int32_t hq, int32_t hkv, int32_t d, float softmax_scale,
+                              const bf1_decode_plan *plan /* host */, void *workspace, void *o, float *lse, void *stream);
 
 /* ---- backward over the same route (Section 4.2's gates include a backward pass with finite
  * Q, K and V gradients) ---------------------------------------------------------------------------
@@ -374,7 +383,9 @@ typedef struct {
     int32_t *seqlens;           /* [batch] cached tokens after the step; may be seqlens_dev itself              */
     int32_t *free_count;        /* [1] free pages after the step; may be free_count_dev itself                  */
     int32_t *cu_tokens;         /* [batch + 1] offsets of the sequences' new tokens: the newest token of a sequence that
-                                   has any is row cu_tokens[s + 1] - 1 (bf1_decode_fwd* want a row per sequence) */
+                                   has any is row cu_tokens[s + 1] - 1 (bf1_decode_fwd_fp8_packed goes by that;
+                                   bf1_decode_fwd and bf1_decode_fwd_fp8 want row s for sequence s, which is the
+                                   same only where every sequence adds one token)                              */
     int32_t *positions;         /* [capacity_tokens] a token's position in its sequence; -1 behind the last one */
     int32_t *slots;             /* [capacity_tokens] page * 64 + row; -1 behind the last one                    */
     int32_t *units;             /* [capacity_units, 4] tokens that share a page, in order: first token, number, page,

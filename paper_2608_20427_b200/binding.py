@@ -27,7 +27,7 @@ EXPORTS = ("bf1_route_capacity", "bf1_plan_route", "bf1_attn_fwd", "bf1_dense_ca
            "bf1_attn_bwd", "bf1_attn_bwd_workspace_bytes", "bf1_shard_needed_blocks", "bf1_plan_route_shard",
            "bf1_shard_needed_blocks_strided", "bf1_plan_route_shard_strided",
            "bf1_rope_turns", "bf1_rope_fwd", "bf1_rope_bwd",
-           "bf1_decode_fp8_workspace_bytes", "bf1_decode_fwd_fp8", "bf1_cache_plan_units", "bf1_plan_cache", "bf1_cache_write",
+           "bf1_decode_fp8_workspace_bytes", "bf1_decode_fwd_fp8", "bf1_decode_fwd_fp8_packed", "bf1_cache_plan_units", "bf1_plan_cache", "bf1_cache_write",
            "bf1_last_error", "bf1_version")
 
 
@@ -147,6 +147,8 @@ def load():
     L.bf1_decode_fp8_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
     L.bf1_decode_fwd_fp8.restype = ctypes.c_int
     L.bf1_decode_fwd_fp8.argtypes = [vp, vp, vp, vp, vp, i32, vp, i32, i32, i32, i32, f32, ctypes.POINTER(_DecodePlanC), vp, vp, vp, vp]
+    L.bf1_decode_fwd_fp8_packed.restype = ctypes.c_int
+    L.bf1_decode_fwd_fp8_packed.argtypes = [vp, i32, vp, vp, vp, vp, vp, i32, vp, i32, i32, i32, i32, f32, ctypes.POINTER(_DecodePlanC), vp, vp, vp, vp]
     L.bf1_last_error.restype = ctypes.c_char_p
     L.bf1_last_error.argtypes = []
     L.bf1_version.restype = ctypes.c_int
@@ -348,12 +350,16 @@ def decode_fp8_workspace(batch: int, hq: int, hkv: int, max_degree: int, d: int,
 
 
 def decode_fwd_fp8(q, k_pages, v_pages, k_scales, v_scales, seqlens, plan: DecodePlan, workspace, scale: Optional[float] = None,
-                   out=None, lse=None, stream=None):
+                   out=None, lse=None, stream=None, cu_tokens=None):
     """bf1_decode_fwd_fp8: decode_fwd over a cache in 8 bits.  q [batch, hq, d] bf16; k_pages / v_pages [pages, 64, hkv, d]
     float8_e4m3fn, k_scales / v_scales [pages, hkv] fp32.  Page lists may be of any length: a dense layer's plan is
-    plan_decode(seqlens, page_table, RouteCfg(64, page_table.shape[1], 0, 0))."""
+    plan_decode(seqlens, page_table, RouteCfg(64, page_table.shape[1], 0, 0)).
+
+    With cu_tokens [batch + 1] (bf1_decode_fwd_fp8_packed) q and out are a step's packed rows [tokens, hq, d], as plan_cache numbers them and
+    cache_write takes them, and lse is [hq, tokens]: the newest token of sequence s is row cu_tokens[s + 1] - 1, and a sequence without a
+    token in the step is passed over.  Without it row s belongs to sequence s."""
     return _host().decode_fp8(q, k_pages, v_pages, k_scales, v_scales, seqlens, ctypes.addressof(plan.c), plan.count, workspace, scale,
-                              out, lse, _stream_ptr(stream))
+                              out, lse, _stream_ptr(stream), cu_tokens)
 
 
 def bwd_workspace(route: Route, total_tokens: int, hq: int, hkv: int, d: int, device) -> torch.Tensor:

@@ -42,14 +42,16 @@ constexpr float kPUp = 32768.f;          // P enters the products times 2^15, so
 enum { kRuns, kWhole, kParts };
 
 struct Decode8Args {
-    const __nv_bfloat16* q;              // [batch, hq, d]
+    const __nv_bfloat16* q;              // [rows, hq, d]
     const float *k_scales, *v_scales;    // [pages, hkv]
     const int32_t *seqlens, *count, *page, *block;
+    const int32_t* cu_tokens;            // [batch + 1] the sequences' new tokens among the rows, or null: row s is sequence s
     int32_t* status;
+    int32_t rows;                        // of q, o and lse
     int32_t max_degree, hq, hkv, num_pages, group, batch;
     float scale_log2;
-    __nv_bfloat16* o;                    // [batch, hq, d]
-    float* lse;                          // [hq, batch]
+    __nv_bfloat16* o;                    // [rows, hq, d]
+    float* lse;                          // [hq, rows]
     int32_t runs;                        // kRuns: per KV head
     int32_t stages, ahead;               // pages in a CTA's ring, and of those asked for at once at the start
     int32_t nctas, share;                // kParts: CTAs to a list, columns (of the heads' G d) that each adds up, a multiple of 32
@@ -64,6 +66,11 @@ struct Decode8Args {
 __device__ __forceinline__ int runs_of(int runs, long long pages, int longest) {
     const long long most = (pages + kD8MinRun - 1) / kD8MinRun;
     return (int)fminf((float)min((long long)runs, most), ceilf(4.f * (float)pages * rsqrtf((float)max(longest, 1))));
+}
+
+// The row of a sequence's newest token; within the arrays whatever stands there by now (pages_of_list has refused others).
+__device__ __forceinline__ int row_of_list(const Decode8Args& a, int s) {
+    return a.cu_tokens ? min(max(a.cu_tokens[s + 1] - 1, 0), a.rows - 1) : s;
 }
 
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, int c0, int c1, int c2, uint32_t bar) {
@@ -117,13 +124,13 @@ __device__ __forceinline__ uint32_t page_chunk(int r, int c) {
 // head's largest value into [2^14, 2^15): what is above 2^-38 of it has all its digits.  f[0], f[1]: what the scores of heads 2 tig and
 // 2 tig + 1 have to be multiplied with (the softmax's scale and log2 e in it).
 template <int D>
-__device__ __forceinline__ void load_queries(const Decode8Args& a, int s, int hbase, uint32_t (&qb)[D / 16][2], float (&f)[2]) {
+__device__ __forceinline__ void load_queries(const Decode8Args& a, int row, int hbase, uint32_t (&qb)[D / 16][2], float (&f)[2]) {
     const int lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
     float x[D / 16][4], top = 0.f;
-    const uint2* row = reinterpret_cast<const uint2*>(a.q + ((size_t)s * a.hq + hbase + (gid < a.group ? gid : 0)) * D);
+    const uint2* head = reinterpret_cast<const uint2*>(a.q + ((size_t)row * a.hq + hbase + (gid < a.group ? gid : 0)) * D);
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) {
-        const uint2 v = gid < a.group ? row[c * 4 + tig] : make_uint2(0u, 0u);
+        const uint2 v = gid < a.group ? head[c * 4 + tig] : make_uint2(0u, 0u);
         x[c][0] = __uint_as_float(v.x << 16);
         x[c][1] = __uint_as_float(v.x & 0xffff0000u);
         x[c][2] = __uint_as_float(v.y << 16);
@@ -299,7 +306,15 @@ __global__ void __launch_bounds__(kD8Threads, kMode == kWhole && D == 64 ? 4 : 3
     const bool reports = kvh == 0 && blockIdx.z == 0;
     auto pages_of_list = [&](int s, bool report) {
         const int n = a.seqlens[s];
-        const int c = max(min(a.count[s], a.max_degree), 0);
+        int c = max(min(a.count[s], a.max_degree), 0);
+        if (a.cu_tokens) {                                           // a sequence without a token in this step has no row
+            const int first = a.cu_tokens[s], end = a.cu_tokens[s + 1];
+            if (end <= first) c = 0;
+            else if (first < 0 || end > a.rows) {
+                if (c > 0 && report) atomicOr(a.status, BF1_DEV_BAD_ROUTE);
+                c = 0;
+            }
+        }
         if (c > 0 && (n < 1 || (n - 1) / kP8 != a.block[s])) {       // the plan belongs to another 64 tokens
             if (report) atomicOr(a.status, BF1_DEV_BAD_ROUTE);
             return 0;
@@ -452,14 +467,16 @@ __global__ void __launch_bounds__(kD8Threads, kMode == kWhole && D == 64 ? 4 : 3
     const int key0 = warp * 16, hbase = kvh * a.group, gid = lane >> 2, tig = lane & 3;
     constexpr int kCols = kHeads * D / kD8Consumers, kPerHead = kD8Consumers / kHeads;
     const int h = tid / kPerHead, c0 = tid % kPerHead * kCols;
-    int stage = 0, parity = 0;
+    int stage = 0, parity = 0, row = 0;
     s = list_of(x0);
+    if constexpr (kMode != kRuns) row = row_of_list(a, s);
     // the part of list s from page x to `end` (of `last`), and the four warps' states merged: (max, sum) and this thread's columns
     auto part = [&](int x, int end, int last, float& m, float& l, float (&out)[kCols]) {
         const int n = a.seqlens[s], tail = n - (n - 1) / kP8 * kP8;
+        if constexpr (kMode == kRuns) row = row_of_list(a, s);
         uint32_t qb[D / 16][2];
         float f[2];
-        load_queries<D>(a, s, hbase, qb, f);
+        load_queries<D>(a, row, hbase, qb, f);
         WarpState<D> w;
         w.clear();
         auto next = [&]() {                                  // waits for a page; its place in the ring
@@ -526,10 +543,10 @@ __global__ void __launch_bounds__(kD8Threads, kMode == kWhole && D == 64 ? 4 : 3
     auto write = [&](float m, float l, const float (&out)[kCols]) {
         if (h >= a.group) return;                            // G = 1: the second head does not exist
         const float inv = 1.f / l;
-        __nv_bfloat16* orow = a.o + ((size_t)s * a.hq + hbase + h) * D + c0;
+        __nv_bfloat16* orow = a.o + ((size_t)row * a.hq + hbase + h) * D + c0;
 #pragma unroll
         for (int c = 0; c < kCols; ++c) orow[c] = __float2bfloat16_rn(out[c] * inv);
-        if (c0 == 0) a.lse[(size_t)(hbase + h) * a.batch + s] = (m + log2f(l)) * 0.6931471805599453f;
+        if (c0 == 0) a.lse[(size_t)(hbase + h) * a.rows + row] = (m + log2f(l)) * 0.6931471805599453f;
     };
     float m, l, out[kCols];
     if constexpr (kMode == kWhole) {
@@ -604,8 +621,8 @@ __global__ void __launch_bounds__(kD8Threads, kMode == kWhole && D == 64 ? 4 : 3
                     if (i0 + i < a.nctas) o = fmaf(wi[i], p[i], o);
             }
             if (hv < a.group) {
-                a.o[((size_t)s * a.hq + hbase + hv) * D + col] = __float2bfloat16_rn(o * (1.f / sum));
-                if (col == 0) a.lse[(size_t)(hbase + hv) * a.batch + s] = (top + log2f(sum)) * 0.6931471805599453f;
+                a.o[((size_t)row * a.hq + hbase + hv) * D + col] = __float2bfloat16_rn(o * (1.f / sum));
+                if (col == 0) a.lse[(size_t)(hbase + hv) * a.rows + row] = (top + log2f(sum)) * 0.6931471805599453f;
             }
         }
     }
@@ -629,6 +646,7 @@ __global__ void __launch_bounds__(kJoinThreads) decode8_join_kernel(const Decode
     auto run_of = [&](long long x) { return (int)(((x + 1) * runs - 1) / total); };   // the last run that begins at or in front of page x
     const int j0 = run_of(first), j1 = run_of(last - 1), parts = j1 - j0 + 1;
     if (parts == 1) return;                                  // whole: written already
+    const int row = row_of_list(a, s);
     auto slot = [&](int j) { return (((size_t)kvh * a.runs + j) * 2 + (j == j0 ? 1 : 0)) * a.group; };
     const int columns = min(a.group * kVec, kJoinColumns), groups = kJoinThreads / columns;
     const int g = tid / columns, column = blockIdx.z * columns + tid % columns, h = column / kVec, c = column % kVec;
@@ -687,8 +705,8 @@ __global__ void __launch_bounds__(kJoinThreads) decode8_join_kernel(const Decode
 #pragma unroll
     for (int i = 1; i < kJoinThreads / 32; ++i) m = fmaxf(m, tops[i][h]), l += ls[i][h];
     const float inv = 1.f / l;
-    *reinterpret_cast<uint2*>(a.o + ((size_t)s * a.hq + kvh * a.group + h) * D + 4 * c) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
-    if (c == 0) a.lse[(size_t)(kvh * a.group + h) * a.batch + s] = (m + log2f(l)) * 0.6931471805599453f;
+    *reinterpret_cast<uint2*>(a.o + ((size_t)row * a.hq + kvh * a.group + h) * D + 4 * c) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+    if (c == 0) a.lse[(size_t)(kvh * a.group + h) * a.rows + row] = (m + log2f(l)) * 0.6931471805599453f;
 }
 
 int make_page_map(CUtensorMap* m, const void* ptr, int64_t pages, int hkv, int d);   // bf1_attn.cu
@@ -738,13 +756,14 @@ extern "C" int64_t bf1_decode_fp8_workspace_bytes(int32_t batch, int32_t hq, int
     return (int64_t)(up16(sizeof(int32_t) * ((size_t)batch + 2)) + parts * (sizeof(float2) + sizeof(float) * d));
 }
 
-extern "C" int bf1_decode_fwd_fp8(const void* q, const void* k_pages, const void* v_pages, const float* k_scales, const float* v_scales,
-                                  int32_t num_pages, const int32_t* seqlens_dev, int32_t batch, int32_t hq, int32_t hkv, int32_t d,
-                                  float softmax_scale, const bf1_decode_plan* plan, void* workspace, void* o, float* lse, void* stream) {
+// cu_tokens_dev null: `rows` is the batch.
+static int decode8(const void* q, int32_t rows, const int32_t* cu_tokens_dev, const void* k_pages, const void* v_pages, const float* k_scales,
+                   const float* v_scales, int32_t num_pages, const int32_t* seqlens_dev, int32_t batch, int32_t hq, int32_t hkv, int32_t d,
+                   float softmax_scale, const bf1_decode_plan* plan, void* workspace, void* o, float* lse, void* stream) {
     if (!q || !k_pages || !v_pages || !k_scales || !v_scales || !seqlens_dev || !plan || !workspace || !o || !lse)
         return fail(BF1_ERR_INVALID_ARG, "a pointer is null");
     if (!plan->count || !plan->page || !plan->block || !plan->status) return fail(BF1_ERR_INVALID_ARG, "a decode-plan pointer is null");
-    if (batch < 0 || num_pages < 1 || hq <= 0 || hkv <= 0) return fail(BF1_ERR_INVALID_ARG, "negative or zero size argument");
+    if (batch < 0 || rows < 0 || num_pages < 1 || hq <= 0 || hkv <= 0) return fail(BF1_ERR_INVALID_ARG, "negative or zero size argument");
     if (hq % hkv != 0) return fail(BF1_ERR_INVALID_ARG, "hq %d is not a multiple of hkv %d", hq, hkv);
     const int group = hq / hkv;
     if (group != 1 && group != 2 && group != 4) return fail(BF1_ERR_UNSUPPORTED, "GQA group size %d: only G = 1, 2 and 4 are supported", group);
@@ -753,7 +772,7 @@ extern "C" int bf1_decode_fwd_fp8(const void* q, const void* k_pages, const void
         return fail(BF1_ERR_INVALID_ARG, "q, k_pages, v_pages, o and workspace must be 16-byte aligned");
     if (plan->max_degree < 1 || batch > 65535 || hkv > 65535 || num_pages > (1 << 25) - 1 || (int64_t)plan->max_degree * std::min(batch, kD8MaxScan) > 0x7fffffffLL)
         return fail(BF1_ERR_UNSUPPORTED, "batch and KV heads up to 65535, pages up to 2^25 - 1, pages of all lists below 2^31");
-    if (batch == 0) return BF1_OK;
+    if (batch == 0 || rows == 0) return BF1_OK;
     Decode8Args a;
     a.q = (const __nv_bfloat16*)q;
     a.k_scales = k_scales;
@@ -762,7 +781,9 @@ extern "C" int bf1_decode_fwd_fp8(const void* q, const void* k_pages, const void
     a.count = plan->count;
     a.page = plan->page;
     a.block = plan->block;
+    a.cu_tokens = cu_tokens_dev;
     a.status = plan->status;
+    a.rows = rows;
     a.max_degree = plan->max_degree;
     a.hq = hq;
     a.hkv = hkv;
@@ -852,4 +873,20 @@ extern "C" int bf1_decode_fwd_fp8(const void* q, const void* k_pages, const void
                                   kJoinThreads, 0,
                                   (cudaStream_t)stream, a));
     return BF1_OK;
+}
+
+extern "C" int bf1_decode_fwd_fp8(const void* q, const void* k_pages, const void* v_pages, const float* k_scales, const float* v_scales,
+                                  int32_t num_pages, const int32_t* seqlens_dev, int32_t batch, int32_t hq, int32_t hkv, int32_t d,
+                                  float softmax_scale, const bf1_decode_plan* plan, void* workspace, void* o, float* lse, void* stream) {
+    return decode8(q, batch, nullptr, k_pages, v_pages, k_scales, v_scales, num_pages, seqlens_dev, batch, hq, hkv, d, softmax_scale, plan, workspace, o, lse,
+                   stream);
+}
+
+extern "C" int bf1_decode_fwd_fp8_packed(const void* q, int32_t tokens, const int32_t* cu_tokens_dev, const void* k_pages, const void* v_pages,
+                                         const float* k_scales, const float* v_scales, int32_t num_pages, const int32_t* seqlens_dev, int32_t batch,
+                                         int32_t hq, int32_t hkv, int32_t d, float softmax_scale, const bf1_decode_plan* plan, void* workspace, void* o,
+                                         float* lse, void* stream) {
+    if (!cu_tokens_dev) return fail(BF1_ERR_INVALID_ARG, "a pointer is null");
+    return decode8(q, tokens, cu_tokens_dev, k_pages, v_pages, k_scales, v_scales, num_pages, seqlens_dev, batch, hq, hkv, d, softmax_scale, plan, workspace, o,
+                   lse, stream);
 }

@@ -255,7 +255,7 @@ void check_table(const at::Tensor& turns, const at::Tensor& like) {
     array_of<const double>(turns, like, at::kDouble, "the rope's table must be on the device of the tensors");
 }
 
-// decode_fp8(q, k_pages, v_pages, k_scales, v_scales, seqlens, plan address, its counts, workspace, scale*, out*, lse*, stream*)
+// decode_fp8(q, k_pages, v_pages, k_scales, v_scales, seqlens, plan address, its counts, workspace, scale*, out*, lse*, stream*, cu_tokens*)
 PyObject* decode_fp8(PyObject* const* a) {
     const at::Tensor &q = tensor(a[0]), &kp = tensor(a[1]), &vp = tensor(a[2]), &ks = tensor(a[3]), &vs = tensor(a[4]), &seqlens = tensor(a[5]),
                      &count = tensor(a[7]), &ws = tensor(a[8]);
@@ -269,18 +269,29 @@ PyObject* decode_fp8(PyObject* const* a) {
     require(ks.dim() == 2 && ks.size(0) == kp.size(0) && ks.size(1) == kp.size(2) && vs.sizes() == ks.sizes(), scales);
     const auto* sp = array_of<const int32_t>(seqlens, q, at::kInt, "seqlens must be a contiguous int32 tensor on the device of q");
     array_of<int32_t>(count, q, at::kInt, "the plan must be on the device of the tensors");
-    require(seqlens.dim() == 1 && seqlens.size(0) == q.size(0) && count.size(0) == q.size(0), "q, seqlens and the plan must be of the same batch");
+    const int32_t* cu = nullptr;
+    if (a[13] != Py_None) {
+        const at::Tensor& t = tensor(a[13]);
+        cu = array_of<const int32_t>(t, q, at::kInt, "cu_tokens must be a contiguous int32 tensor on the device of q");
+        require(seqlens.dim() == 1 && seqlens.size(0) == count.size(0) && t.dim() == 1 && t.size(0) == count.size(0) + 1,
+                "seqlens and the plan must be of the same batch, cu_tokens [batch + 1]");
+        require(q.size(0) <= INT32_MAX, "too many rows");
+    } else {
+        require(seqlens.dim() == 1 && seqlens.size(0) == q.size(0) && count.size(0) == q.size(0), "q, seqlens and the plan must be of the same batch");
+    }
     const auto* plan = address<const bf1_decode_plan>(a[6]);
     const float scale = scale_of(a[9]);
-    const int32_t batch = q.size(0), hq = q.size(1), d = q.size(2), pages = kp.size(0), hkv = kp.size(2);
+    const int32_t rows = q.size(0), batch = seqlens.size(0), hq = q.size(1), d = q.size(2), pages = kp.size(0), hkv = kp.size(2);
     void* wp = array_of<void>(ws, q, at::kByte, "the workspace must be a byte tensor on the device of q");
     require(ws.numel() >= bf1_decode_fp8_workspace_bytes(batch, hq, hkv, plan->max_degree, d), "the workspace is too small: see decode_fp8_workspace");
     const at::Tensor out = a[10] == Py_None ? at::empty(q.sizes(), q.options()) : tensor(a[10]);
-    const at::Tensor lse = a[11] == Py_None ? lse_like(q, hq, batch) : tensor(a[11]);
-    require(out.sizes() == q.sizes() && lse.dim() == 2 && lse.size(0) == hq && lse.size(1) == batch, "out must have the shape of q, lse must be [hq, batch]");
+    const at::Tensor lse = a[11] == Py_None ? lse_like(q, hq, rows) : tensor(a[11]);
+    require(out.sizes() == q.sizes() && lse.dim() == 2 && lse.size(0) == hq && lse.size(1) == rows, "out must have the shape of q, lse must be [hq, rows of q]");
     void* op = array_of<void>(out, q, at::kBFloat16, "out must be a contiguous bf16 tensor on the device of q");
     auto* lp = array_of<float>(lse, q, at::kFloat, "lse must be a contiguous fp32 tensor on the device of q");
-    if (batch > 0)
+    if (batch > 0 && rows > 0 && cu)
+        call([&] { return bf1_decode_fwd_fp8_packed(qp, rows, cu, kpp, vpp, ksp, vsp, pages, sp, batch, hq, hkv, d, scale, plan, wp, op, lp, place.stream); });
+    else if (batch > 0 && rows > 0)
         call([&] { return bf1_decode_fwd_fp8(qp, kpp, vpp, ksp, vsp, pages, sp, batch, hq, hkv, d, scale, plan, wp, op, lp, place.stream); });
     return pair(out, lse);
 }
@@ -430,7 +441,7 @@ PyMethodDef g_methods[] = {
     BF1_ENTRY(backward, 12),
     BF1_ENTRY(plan_decode, 5),
     BF1_ENTRY(decode, 10),
-    BF1_ENTRY(decode_fp8, 13),
+    BF1_ENTRY(decode_fp8, 14),
     BF1_ENTRY(rope, 9),
     BF1_ENTRY(plan_cache, 11),
     BF1_ENTRY(cache_write, 13),

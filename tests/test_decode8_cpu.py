@@ -50,3 +50,17 @@ def test_refusals():
     for args in ((-1, 2, 1, 1, 64), (1, 3, 2, 1, 64), (1, 2, 1, 0, 64), (1, 2, 1, 1, 0), (1, 0, 1, 1, 64)):
         assert lib.bf1_decode_fp8_workspace_bytes(*args) == -1
     assert 16 <= lib.bf1_decode_fp8_workspace_bytes(1024, 32, 8, 10 ** 6, 128) < 8 << 20
+
+
+def test_refusals_of_packed_rows():
+    lib = bf1.load()
+    f = ctypes.c_void_p(0x1000)
+    plan = ctypes.byref(binding._DecodePlanC(11, 0x1000, 0x1000, 0x1000, 0x1000))
+
+    def call(q=f, rows=4, cu=f, batch=2, hq=2, hkv=1, d=64, o=f, lse=f):
+        return lib.bf1_decode_fwd_fp8_packed(q, rows, cu, f, f, f, f, 1, f, batch, hq, hkv, d, 0.0, plan, f, o, lse, None)
+
+    assert call(batch=0) == 0 and call(rows=0) == 0                 # nothing to do, nothing launched
+    assert call(cu=None) == -1 and call(q=None) == -1 and call(o=None) == -1 and call(lse=None) == -1
+    assert call(rows=-1) == -1 and call(batch=-1) == -1 and call(hq=3, hkv=2) == -1
+    assert call(hq=8) == -2 and call(d=96) == -2 and call(batch=65536) == -2

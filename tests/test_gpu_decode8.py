@@ -449,3 +449,132 @@ def test_pages_of_small_weights_and_large_values(lens, hq, hkv, d):
                     c.vs[p] = 2.0 ** -47
         out, lse, _ = run(c, q)
         check_beside(c, q, out, lse)
+
+
+# ---- a step's packed rows ------------------------------------------------------------------------------------------------------------
+def packed(counts, spare=0):
+    cu = np.concatenate([[0], np.cumsum(counts)])
+    return torch.tensor(cu, dtype=torch.int32, device=DEV), int(cu[-1]) + spare
+
+
+@pytest.mark.parametrize("lens,counts,hq,hkv,d,dense", [([70, 300, 0, 64, 1, 129], [1, 0, 0, 3, 1, 129], 4, 2, 64, False), ([20000, 65, 9000, 3], [0, 1, 1, 2], 16, 8, 128, True),
+                                                        ([26000, 500, 27000, 1], [1, 0, 1, 1], 2, 1, 64, True), ([300] * 200, [1, 0, 2, 1] * 50, 2, 1, 128, False),
+                                                        ([100, 200], [0, 0], 2, 2, 64, False), ([2000] * 90, [0, 1, 1] * 30, 8, 2, 64, True)],
+                         ids=["parts", "runs", "runs-64", "whole", "none", "runs-many"])
+def test_packed_rows(lens, counts, hq, hkv, d, dense):
+    """Every sequence with tokens in the step is decoded from the row of its newest one, the others are passed over."""
+    c = Cache(lens, hkv, d, dense, seed=19)
+    cu, rows = packed(counts, spare=2)
+    q = queries(rows, hq, d, 20).to(DEV)
+    lens_d = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    plan = bf1.plan_decode(lens_d, c.table.to(DEV), c.cfg)
+    ws = bf1.decode_fp8_workspace(len(lens), hq, hkv, plan.max_degree, d, DEV)
+    ws.fill_(0xff)
+    out, lse = torch.full_like(q, float("nan")), torch.full((hq, rows), float("nan"), device=DEV)
+    args = [t.to(DEV) for t in (c.kp, c.vp, c.ks, c.vs)]
+    got = bf1.decode_fwd_fp8(q, *args, lens_d, plan, ws, out=out, lse=lse, cu_tokens=cu)
+    assert got[0] is out and got[1] is lse and plan.status.item() == 0
+    live = [s for s, n in enumerate(counts) if n > 0 and lens[s] > 0]
+    at = [int(cu[s + 1]) - 1 for s in live]
+    c.lens = [n if s in live else 0 for s, n in enumerate(lens)]
+    mine = torch.zeros((len(lens), hq, d), dtype=torch.bfloat16)
+    mine[live] = q[at].cpu()
+    spread, spread_lse = (torch.full(s, float("nan"), dtype=t) for s, t in ((mine.shape, torch.bfloat16), ((hq, len(lens)), torch.float32)))
+    spread[live], spread_lse[:, live] = out[at].cpu(), lse[:, at].cpu()
+    c.lists = [x if n else [] for x, n in zip(c.lists, c.lens)]
+    check(c, mine, spread, spread_lse)
+    others = [r for r in range(rows) if r not in at]
+    assert torch.isnan(out[others]).all() and torch.isnan(lse[:, others]).all()
+    own = bf1.decode_fwd_fp8(q, *args, lens_d, plan, ws, cu_tokens=cu)                 # with results of its own
+    assert torch.equal(own[0][at], out[at]) and torch.equal(own[1][:, at], lse[:, at])
+
+
+def test_packed_rows_outside_the_arrays_are_refused():
+    c = Cache([100, 200, 300], 1, 64, False, seed=21)
+    lens = torch.tensor(c.lens, dtype=torch.int32, device=DEV)
+    args = [t.to(DEV) for t in (c.kp, c.vp, c.ks, c.vs)]
+    q = queries(3, 2, 64, 22).to(DEV)
+    ws = bf1.decode_fp8_workspace(3, 2, 1, 17, 64, DEV)
+    plan = bf1.plan_decode(lens, c.table.to(DEV), c.cfg)
+    want = bf1.decode_fwd_fp8(q, *args, lens, plan, ws)[0]
+    for offsets, good in (([0, 1, 4, 3], [0]), ([-1, 1, 2, 3], [1, 2]), ([0, 1, 2, 2 ** 31 - 1], [0, 1]), ([-5, -2, -1, 0], [])):
+        plan = bf1.plan_decode(lens, c.table.to(DEV), c.cfg)
+        out = torch.full_like(q, float("nan"))
+        bf1.decode_fwd_fp8(q, *args, lens, plan, ws, out=out, cu_tokens=torch.tensor(offsets, dtype=torch.int32, device=DEV))
+        assert plan.status.item() == 8 and torch.equal(out[good], want[good])
+        assert torch.isnan(out[[s for s in range(3) if s not in good]]).all()
+
+
+def test_refusals_of_packed_rows():
+    c = Cache([100], 1, 64, False, seed=12)
+    q, kp, vp, ks, vs = (t.to(DEV) for t in (queries(3, 2, 64, 12), c.kp, c.vp, c.ks, c.vs))
+    lens = torch.tensor([100], dtype=torch.int32, device=DEV)
+    plan = bf1.plan_decode(lens, c.table.to(DEV), c.cfg)
+    ws = bf1.decode_fp8_workspace(1, 2, 1, plan.max_degree, 64, DEV)
+    cu = torch.tensor([0, 3], dtype=torch.int32, device=DEV)
+    f = lambda q=q, lens=lens, **kw: bf1.decode_fwd_fp8(q, kp, vp, ks, vs, lens, plan, ws, **kw)  # noqa: E731
+    for bad in (lambda: f(), lambda: f(cu_tokens=cu[:1]), lambda: f(cu_tokens=cu.long()), lambda: f(cu_tokens=cu.cpu()), lambda: f(cu_tokens=cu[None]),
+                lambda: f(lens=torch.cat((lens, lens)), cu_tokens=cu), lambda: f(cu_tokens=cu, out=torch.zeros_like(q[:1])), lambda: f(cu_tokens=cu, lse=torch.zeros((2, 1), device=DEV))):
+        with pytest.raises(AssertionError):
+            bad()
+    with pytest.raises(TypeError):
+        f(cu_tokens=[0, 3])
+    o, lse = f(q=q[:0], cu_tokens=torch.zeros(2, dtype=torch.int32, device=DEV))
+    assert o.shape == (0, 2, 64) and lse.shape == (2, 0)
+
+
+@pytest.mark.parametrize("dense", [False, True], ids=["route", "dense"])
+def test_a_serving_step_with_idle_and_released_sequences(dense):
+    """The step of a serving loop, captured: sequences wait, end and begin again, each is decoded with its own query.  Against 64 bits over
+    the numbers that the cache holds, rows of nobody left as they were."""
+    hq, hkv, d, pages, batch = 4, 2, 64, 60, 5
+    g = torch.Generator().manual_seed(23)
+    rng = np.random.default_rng(23)
+    rope = bf1.plan_rope(bf1.RopeCfg(64), DEV)
+    route = bf1.RouteCfg(**DENSE) if dense else bf1.RouteCfg()
+    kp, vp = (torch.full((pages, 64, hkv, d), 0x7f, dtype=torch.uint8, device=DEV).view(E4M3) for _ in range(2))
+    ks, vs = (torch.full((pages, hkv), float("nan"), device=DEV) for _ in range(2))
+    lens = torch.zeros(batch, dtype=torch.int32, device=DEV)
+    new = torch.zeros(batch, dtype=torch.int32, device=DEV)
+    table = torch.full((batch, 10), -1, dtype=torch.int32, device=DEV)
+    stack, count = torch.arange(pages, dtype=torch.int32, device=DEV), torch.tensor([pages], dtype=torch.int32, device=DEV)
+    rows = 90
+    step = bf1.CachePlan.empty(batch, rows, DEV)
+    lists = bf1.plan_decode(lens, table, route)
+    ws = bf1.decode_fp8_workspace(batch, hq, hkv, lists.max_degree, d, DEV)
+    q, k, v = (torch.zeros((rows, h, d), dtype=torch.bfloat16, device=DEV) for h in (hq, hkv, hkv))
+    turned, out, lse = torch.zeros_like(q), torch.zeros_like(q), torch.zeros((hq, rows), device=DEV)
+
+    def body():
+        bf1.plan_cache(lens, new, table, pages, rows, stack, count, plan=step, seqlens_out=lens, free_count_out=count)
+        bf1.plan_decode(lens, table, route, plan=lists)
+        bf1.cache_write(k, v, kp, vp, step, ks, vs, rope=rope, q=q, out_q=turned)
+        bf1.decode_fwd_fp8(turned, kp, vp, ks, vs, lens, lists, ws, out=out, lse=lse, cu_tokens=step.cu_tokens)
+
+    body()                                                          # adds nothing
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        body()
+    held = [0] * batch
+    for i in range(40):
+        counts = [int(rng.choice([1, 1, 0, -1 if n else 0, 40])) if i else 60 - 20 * s * (s < 3) for s, n in enumerate(held)]
+        while sum(max(n, 0) for n in counts) > rows:
+            counts[counts.index(max(counts))] = 1
+        new.copy_(torch.tensor(counts, dtype=torch.int32))
+        for t in (q, k, v):
+            t.copy_(torch.randn(t.shape, generator=g).to(torch.bfloat16))
+        out.fill_(float("nan"))
+        lse.fill_(float("nan"))
+        graph.replay()
+        held = [0 if n < 0 else old + n for n, old in zip(counts, held)]
+        assert step.status.item() == 0 and lists.status.item() == 0 and lens.tolist() == held
+        cu = step.cu_tokens.tolist()
+        live = [s for s, n in enumerate(counts) if n > 0]
+        at = [cu[s + 1] - 1 for s in live]
+        c = Cache.__new__(Cache)
+        c.kp, c.vp, c.ks, c.vs = (t.cpu() for t in (kp, vp, ks, vs))
+        c.lens = [held[s] for s in live]
+        c.lists = [[int(table[s, b]) for b in logical(held[s], dense)] for s in live]
+        check(c, turned[at].cpu(), out[at], lse[:, at])
+        others = [r for r in range(rows) if r not in at]
+        assert torch.isnan(out[others]).all() and torch.isnan(lse[:, others]).all()
