@@ -73,6 +73,9 @@ __device__ __forceinline__ int row_of_list(const Decode8Args& a, int s) {
     return a.cu_tokens ? min(max(a.cu_tokens[s + 1] - 1, 0), a.rows - 1) : s;
 }
 
+// A launch on this status word has given up a wait: nothing is done until a plan clears it.
+__device__ __forceinline__ bool given_up(const Decode8Args& a) { return *a.status & BF1_DEV_WAIT_TIMEOUT; }
+
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, int c0, int c1, int c2, uint32_t bar) {
     asm volatile(
         "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
@@ -323,6 +326,7 @@ __global__ void __launch_bounds__(kD8Threads, kMode == kWhole && D == 64 ? 4 : 3
     };
     // ---- this CTA's pages: x0 .. x1 - 1 of the row (kRuns), or of its list -------------------------------------------------------------
     int s = 0, x0 = 0, x1 = 0, count = 0, held[2] = {-1, -1};
+    bool dead = false;                                               // nothing may be written of this list
     if constexpr (kMode != kRuns) {
         s = blockIdx.y;
         if (warp == kD8Consumers / 32)                               // the list is asked for together with its length
@@ -330,15 +334,21 @@ __global__ void __launch_bounds__(kD8Threads, kMode == kWhole && D == 64 ? 4 : 3
             for (int i = 0; i < 2; ++i)
                 if (lane + 32 * i < a.max_degree) held[i] = a.page[(size_t)s * a.max_degree + lane + 32 * i];
         // read once, since threads that disagreed would not meet at the barriers, and not by the thread that sets these up
-        if (tid == 32) list_count = pages_of_list(s, reports);
+        if (tid == 32) {
+            const bool stopped = given_up(a);                        // (asked for with the length, not in front of it)
+            const int c = pages_of_list(s, reports);
+            list_count = stopped ? -1 : c;
+        }
         __syncthreads();                                             // the barriers are there
-        count = list_count;
+        dead = list_count < 0;
+        count = max(list_count, 0);
         x0 = kMode == kParts ? blockIdx.z * count / a.nctas : 0;
         x1 = kMode == kParts ? (blockIdx.z + 1) * count / a.nctas : count;
         if (kMode == kWhole && count == 0) return;
         if constexpr (kMode == kParts) cluster_arrive_relaxed();     // (waited for in front of the first store to another CTA)
     } else {
         const int per = (a.batch + kD8Threads - 1) / kD8Threads, lo = min(tid * per, a.batch), hi = min(lo + per, a.batch);
+        if (tid == kD8Threads - 1) list_count = given_up(a) ? -1 : 0;        // (by a warp that has nothing to look up here unless lists are many)
         int sum = 0, longest = 0;
         for (int i = lo; i < hi; ++i) {
             const int c = pages_of_list(i, kvh == 0 && blockIdx.y == 0);
@@ -368,7 +378,7 @@ __global__ void __launch_bounds__(kD8Threads, kMode == kWhole && D == 64 ? 4 : 3
         __syncthreads();
         const long long total = bases[a.batch];
         const int runs = runs_of(a.runs, total, longest);
-        if ((int)blockIdx.y < runs && total > 0) {
+        if ((int)blockIdx.y < runs && total > 0 && list_count == 0) {
             x0 = (int)(total * blockIdx.y / runs);
             x1 = (int)(total * (blockIdx.y + 1) / runs);
         }
@@ -540,8 +550,10 @@ __global__ void __launch_bounds__(kD8Threads, kMode == kWhole && D == 64 ? 4 : 3
             for (int c = 0; c < kCols; ++c) out[c] = fmaf(by, st.o[i][h][c0 + c], out[c]);
         }
     };
+    // (read behind a barrier of the four warps that part() ends with: all of them see what one of them, or the copying warp it waited for, has set)
+    auto gave_up = [&]() { return *const_cast<const volatile int*>(&abort_flag) != 0; };
     auto write = [&](float m, float l, const float (&out)[kCols]) {
-        if (h >= a.group) return;                            // G = 1: the second head does not exist
+        if (h >= a.group || gave_up()) return;               // G = 1: the second head does not exist
         const float inv = 1.f / l;
         __nv_bfloat16* orow = a.o + ((size_t)row * a.hq + hbase + h) * D + c0;
 #pragma unroll
@@ -559,7 +571,7 @@ __global__ void __launch_bounds__(kD8Threads, kMode == kWhole && D == 64 ? 4 : 3
             part(x - first, end - first, last - first, m, l, out);
             if (x == first && end == last) {
                 write(m, l, out);
-            } else if (h < a.group) {
+            } else if (h < a.group && !gave_up()) {          // (the join does not read them then)
                 // a run cuts at most two lists: the one it begins in and the one it ends in
                 const size_t slot = (((size_t)kvh * a.runs + blockIdx.y) * 2 + (x == first ? 1 : 0)) * a.group + h;
 #pragma unroll
@@ -572,8 +584,9 @@ __global__ void __launch_bounds__(kD8Threads, kMode == kWhole && D == 64 ? 4 : 3
     } else {
         if (x0 < x1) {
             part(x0, x1, count, m, l, out);
+            if (gave_up()) m = NAN;                          // (a maximum is never NaN: it tells the others)
         } else {                                             // zeros, under a weight of zero
-            m = -INFINITY;
+            m = dead ? NAN : -INFINITY;
             l = 0.f;
 #pragma unroll
             for (int c = 0; c < kCols; ++c) out[c] = 0.f;
@@ -599,6 +612,7 @@ __global__ void __launch_bounds__(kD8Threads, kMode == kWhole && D == 64 ? 4 : 3
             const float2* sums = reinterpret_cast<const float2*>(behind) + hv;                                       // [CTA][kHeads]
             const float* parts = reinterpret_cast<const float*>(behind + (gather_at - sums_at)) + (v - v0);           // [CTA][share]
             const float2 ml = lane < a.nctas ? sums[lane * kHeads] : make_float2(-INFINITY, 0.f);
+            if (__any_sync(0xffffffffu, ml.x != ml.x)) continue;              // a part is missing
             float top = ml.x;
 #pragma unroll
             for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
@@ -640,6 +654,7 @@ __global__ void __launch_bounds__(kJoinThreads) decode8_join_kernel(const Decode
     __shared__ float tops[kJoinThreads / 32][4], ls[kJoinThreads / 32][4];
     pdl_wait();
     const int kvh = blockIdx.x, s = blockIdx.y, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const bool stopped = given_up(a);                        // (needed in front of the store only: unlike the bases it comes from memory)
     const long long total = a.bases[a.batch], first = a.bases[s], last = a.bases[s + 1];
     if (first == last) return;
     const long long runs = a.bases[a.batch + 1];
@@ -695,7 +710,7 @@ __global__ void __launch_bounds__(kJoinThreads) decode8_join_kernel(const Decode
     }
     sums[tid] = o;
     __syncthreads();
-    if (g > 0) return;
+    if (g > 0 || stopped) return;
     for (int i = 1; i < groups; ++i) {
         const float4 v = sums[i * columns + tid];
         o.x += v.x, o.y += v.y, o.z += v.z, o.w += v.w;

@@ -578,3 +578,19 @@ def test_a_serving_step_with_idle_and_released_sequences(dense):
         check(c, turned[at].cpu(), out[at], lse[:, at])
         others = [r for r in range(rows) if r not in at]
         assert torch.isnan(out[others]).all() and torch.isnan(lse[:, others]).all()
+
+
+@pytest.mark.parametrize("lens,hq,hkv,d", [([300] * 3, 4, 2, 64), ([256] * 160, 2, 1, 128), ([26000, 70], 2, 1, 128), ([100], 2, 2, 64)], ids=["parts", "whole", "runs", "one"])
+def test_nothing_is_done_behind_a_wait_that_ran_out(lens, hq, hkv, d):
+    """The bit that a launch leaves behind when it has given up a wait: later ones on its status word write nothing, until a plan clears it."""
+    c = Cache(lens, hkv, d, True, seed=24)
+    q = queries(len(lens), hq, d, 24)
+    lens_d = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    plan = bf1.plan_decode(lens_d, c.table.to(DEV), c.cfg)
+    plan.status.fill_(4)
+    out, lse, _ = run(c, q, plan=plan)
+    assert torch.isnan(out).all() and torch.isnan(lse).all() and plan.status.item() == 4
+    bf1.plan_decode(lens_d, c.table.to(DEV), c.cfg, plan=plan)
+    out, lse, _ = run(c, q, plan=plan)
+    assert plan.status.item() == 0
+    check(c, q, out, lse)
