@@ -437,7 +437,8 @@ def plan_rope(cfg: RopeCfg, device) -> Rope:
 def rope_fwd(q, k, positions, rope: Rope, out_q=None, out_k=None, stream=None):
     """bf1_rope_fwd: (q, k) with their heads rotated to `positions` (int32, one per token; negative: padding, whose output rows
     are not written).  q [T, hq, d], k [T, hkv, d] or None, bf16; rows and heads may be strided (parts of one projection's output), the
-    outputs too, and they may be the inputs themselves.  Without out_q / out_k new contiguous tensors are made."""
+    outputs too, and they may be the inputs themselves.  Without out_q / out_k new contiguous tensors are made; out_k without k is
+    refused."""
     return _host().rope(0, q, k, positions, ctypes.addressof(rope.c), rope.turns, out_q, out_k, _stream_ptr(stream))
 
 

@@ -302,6 +302,7 @@ PyObject* rope(PyObject* const* a) {
     const at::Tensor &q = tensor(a[1]), &k = keys ? tensor(a[2]) : q, &pos = tensor(a[3]);
     const auto* table = address<const bf1_rope>(a[4]);
     const char* const what = "q, k and their outputs must be 3-d bf16 tensors on one CUDA device, the last dimension contiguous";
+    require(keys || a[7] == Py_None, "out_k is given without k");
     const Place place(q, a[8]);
     check_table(tensor(a[5]), q);
     const bf1_rows qr = rows_of(q, q, what), kr = rows_of(k, q, what);
@@ -365,6 +366,8 @@ PyObject* plan_cache(PyObject* const* a) {
 // cache_write(k, v, k_pages, v_pages, plan address, its status, k_scales*, v_scales*, rope address*, its table*, q*, out_q*, stream*)
 PyObject* cache_write(PyObject* const* a) {
     const at::Tensor &k = tensor(a[0]), &v = tensor(a[1]), &kp = tensor(a[2]), &vp = tensor(a[3]);
+    const bool queries = a[10] != Py_None;
+    require(queries || a[11] == Py_None, "out_q is given without q");
     const Place place(k, a[12]);
     const char* const what = "k, v, q and out_q must be 3-d bf16 tensors on one CUDA device, the last dimension contiguous";
     const bf1_rows kr = rows_of(k, k, what), vr = rows_of(v, k, what);
@@ -390,7 +393,6 @@ PyObject* cache_write(PyObject* const* a) {
         rope = address<const bf1_rope>(a[8]);
         check_table(tensor(a[9]), k);
     }
-    const bool queries = a[10] != Py_None;
     bf1_rows qr = {}, oq = {};
     at::Tensor out_q;
     int32_t hq = 0;

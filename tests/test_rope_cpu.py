@@ -4,6 +4,7 @@ import math
 
 import numpy as np
 import pytest
+import torch
 
 import paper_2608_20427_b200 as bf1
 from oracle import cache_oracle as C
@@ -70,3 +71,16 @@ def test_refusals():
     assert call(q=rows(row=12)) == -1 and call(k=rows(head=65)) == -1
     assert call(r=rope(dim=128)) == -2 and call(r=rope(dim=24)) == -2 and call(r=rope(layout=2)) == -1 and call(r=rope(turns=None)) == -1
     assert call(q=rows(0x2000, row=256)) == -1 and b"in place" in lib.bf1_last_error()
+
+
+def test_outputs_without_their_inputs_are_refused():
+    """Before anything else is looked at, the device included."""
+    q = torch.zeros((2, 1, 64), dtype=torch.bfloat16)
+    pos = torch.zeros(2, dtype=torch.int32)
+    rope = bf1.plan_rope(bf1.RopeCfg(64), "cpu")
+    for call in (bf1.rope_fwd, bf1.rope_bwd):
+        with pytest.raises(AssertionError, match="out_k is given without k"):
+            call(q, None, pos, rope, out_k=torch.zeros_like(q))
+    pages = torch.zeros((1, 64, 1, 64), dtype=torch.bfloat16)
+    with pytest.raises(AssertionError, match="out_q is given without q"):
+        bf1.cache_write(q, q, pages, pages, bf1.CachePlan.empty(1, 2, "cpu"), rope=rope, out_q=torch.zeros_like(q))
