@@ -7,12 +7,12 @@
 // sum, O) through shared memory.  The list of a dense layer has hundreds of pages, and lists are of all lengths: then the work is not dealt by lists, but for
 // every KV head the pages of all of them stand in one row, which is cut into equal runs, one to a CTA, as many as the SMs hold at once.  The CTAs that read
 // the heads of one page run side by side, so that its rows are fetched together.  A list that a cut goes through is left as partial results, which a second
-// small kernel adds up in list order.  Measured: 24 lists of up to 32K tokens, 16 query / 8 KV heads, d = 128, 842 MB: 130 us, 6.45 TB/s, a copy's rate; one
-// sequence of 100K tokens 39.8 us (floor 31.7), 32 along the route 12.6 (7.2), one along the route 4.3.
+// small kernel adds up in list order.  Measured: 24 lists of up to 32K tokens, 16 query / 8 KV heads, d = 128, 842 MB: 131 to 132 us, 6.4 TB/s, 98 to 99 % of
+// a copy's rate; one sequence of 100K tokens 40.4 us (floor 31.7), 32 along the route 12.5 (7.2), one along the route 4.2.
 //
 // In a CTA one warp asks for pages by TMA into a ring, and four warps take 16 keys of every page each.  The numbers of the cache are the A
 // operand of m16n8k16 (16 keys or 16 dimensions to a row, the heads are the eight columns): widened from e4m3 to f16, which is
-// exact, two at a time.  q, eight bits of fraction in bf16, is exact in f16 too once it is scaled to the head's largest value; P in f16 is rounded
+// exact, two at a time.  q, eight significant bits in bf16, is exact in f16 too, down to 2^-31 of the head's largest value, once it is scaled to that; P in f16 is rounded
 // by 2^-11, an eighth of what bf16 would cost.  So that this holds for small weights too, P is made against the largest of the sixteen keys (not of the list) and
 // enters times 2^15: f16 has all its digits down to 2^-29 of that one, and steps of 2^-39 of it below.  (Against the list's largest and times 1, a key 17 nats
 // above the others took all weight from those that its warp saw: with a value of zero it left nothing but rounding.)  Scales stay outside of the
@@ -124,7 +124,8 @@ __device__ __forceinline__ uint32_t page_chunk(int r, int c) {
 
 // The queries of a list's heads as the B operand of the scores: column gid is head gid, and the four values that a lane holds of
 // chunk c are the dimensions 16 c + 4 tig .. + 3, the order in which ldmatrix hands out K's bytes.  Scaled by a power of two that puts the
-// head's largest value into [2^14, 2^15): what is above 2^-38 of it has all its digits.  f[0], f[1]: what the scores of heads 2 tig and
+// head's largest value into [2^14, 2^15): what is above 2^-31 of it has all its digits, and what is
+// below half of 2^-38 is zero.  f[0], f[1]: what the scores of heads 2 tig and
 // 2 tig + 1 have to be multiplied with (the softmax's scale and log2 e in it).
 template <int D>
 __device__ __forceinline__ void load_queries(const Decode8Args& a, int row, int hbase, uint32_t (&qb)[D / 16][2], float (&f)[2]) {

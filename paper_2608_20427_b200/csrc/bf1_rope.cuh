@@ -15,8 +15,8 @@ struct RopeTable {
 };
 
 // (cos, sin) of a pair's angle, times the magnitude.  The angle is position * turns in 64 bits, of which only the part of a turn
-// counts: exact to 2^-53 of the whole, so that a position of 2^31 still has 1e-7 of a radian, where 32 bits lose all of it
-// beyond 2^24 turns.  In 32 bits the sine and cosine are those of the rounded angle, corrected by their slopes times what the rounding
+// counts: table and product are each off by 2^-53 of the whole at most, so that a position of 2^31 still has its angle to 4e-7 of a radian (at a
+// pair of one radian per position), where 32 bits lose all of it beyond 2^24 turns.  In 32 bits the sine and cosine are those of the rounded angle, corrected by their slopes times what the rounding
 // took (which would be as large as their own error).  In 64 bits a call costs 2.5 times as much: it is for numbers that are rounded
 // to three bits of fraction next, where an error of 2^-24 may turn a tie.
 __device__ __forceinline__ double rope_half_turns(const RopeTable& r, int position, int pair) {
@@ -48,7 +48,8 @@ __device__ __forceinline__ uint4 pack_bf16x8(const float (&x)[8]) {
     return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
 }
 
-// One pair turned.  The products are rounded in a stated order, so that every kernel gives the same bits.
+// One pair turned.  The products are rounded in a stated order, so that every kernel gives the same bits (of 32-bit angles; the
+// one below is for those of 64 bits: single tokens, or a few that share a page, into pages of 8 bits).
 __device__ __forceinline__ void rope_turn(float& x, float& y, float c, float s) {
     const float p = x, q = y;
     x = __fmaf_rn(p, c, -__fmul_rn(q, s));
