@@ -594,3 +594,25 @@ def test_nothing_is_done_behind_a_wait_that_ran_out(lens, hq, hkv, d):
     out, lse, _ = run(c, q, plan=plan)
     assert plan.status.item() == 0
     check(c, q, out, lse)
+
+
+def test_the_most_lists_that_are_cut():
+    """1024 lists of up to 29 pages are dealt in runs, 1025 walked whole: the workspace, which runs alone write to, says so.  The same data on both sides."""
+    rng = np.random.default_rng(25)
+    lens = [int(x) for x in rng.integers(0, 1850, 1025)]
+    lens[3] = 1850
+    c = Cache(lens, 1, 64, True, seed=25)
+    q = queries(1025, 2, 64, 25)
+    args = [t.to(DEV) for t in (c.kp, c.vp, c.ks, c.vs)]
+    results = []
+    for batch in (1024, 1025):
+        lens_d = torch.tensor(lens[:batch], dtype=torch.int32, device=DEV)
+        plan = bf1.plan_decode(lens_d, c.table[:batch].contiguous().to(DEV), c.cfg)
+        ws = torch.full_like(bf1.decode_fp8_workspace(1024, 2, 1, plan.max_degree, 64, DEV), 0x5a)
+        out, lse = torch.full((batch, 2, 64), float("nan"), dtype=torch.bfloat16, device=DEV), torch.full((2, batch), float("nan"), device=DEV)
+        bf1.decode_fwd_fp8(q[:batch].to(DEV), *args, lens_d, plan, ws, out=out, lse=lse)
+        assert plan.status.item() == 0 and ws.ne(0x5a).any().item() == (batch == 1024)
+        results.append((out, lse))
+    check(c, q, *results[1])
+    c.lens, c.lists = lens[:1024], c.lists[:1024]
+    check(c, q[:1024], *results[0])
